@@ -34,7 +34,8 @@
  *    on a stream of another priority or with a CU mask,
  *    and while a capture that has not ended holds another call of the handle
  *    with one stream and not this one).
- *  - Results are deterministic: no atomics, every reduction in a fixed order.
+ *  - Results are deterministic: every reduction has a fixed order, nothing is
+ *    added atomically to memory that two lanes share.
  *    A call whose branches run one after the other (see above) takes a
  *    parameter-gradient kernel that sums the contraction index in another
  *    fixed order than a call whose branches run side by side does: outputs
@@ -52,7 +53,8 @@
 extern "C" {
 #endif
 
-enum { PE_F32 = 0, PE_BF16 = 1 };
+/* PE_CKPT: an activation checkpoint in 8 bits (pe_ckpt_pack), where an argument says that it may be one. */
+enum { PE_F32 = 0, PE_BF16 = 1, PE_CKPT = 2 };
 
 /* Block orderings of Figure 1.  The sub-operations and parameters are the same; only the place of
  * the outer product mean differs.
@@ -137,6 +139,7 @@ typedef struct pe_ctx_entry {
  * while capturing.                                                            */
 int pe_create(pe_handle** h);
 int pe_destroy(pe_handle* h);
+int pe_handle_device(const pe_handle* h);   /* the device that was current in pe_create */
 
 /* Options.  PE_OPT_BRANCHES: bit 0 = run the MSA branch (+ outer product
  * mean), bit 1 = run the pair branch; default 3.  With a branch disabled its
@@ -296,8 +299,88 @@ int pe_stack_fwd_bwd(pe_handle* h,
                      void* workspace, size_t workspace_bytes,
                      void* stream_msa, void* stream_pair);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators around the trunk: what goes into it (recycled representations through a layer norm,
+ * relative positions) and what is kept of it (checkpoints in 8 bits).
+ *
+ * As for the block: device pointers, buffers and workspace are the caller's, calls only enqueue work
+ * on `stream` (NULL = default stream), allocate nothing, may be captured into a HIP graph, and repeat
+ * bit for bit.  Arguments are validated before anything is launched; pe_last_error has the text of a
+ * refusal.  The current device has to be the handle's (PE_ERR_ARG).  A tensor [rows][c] has a row stride
+ * ld >= c in elements; its buffer is the span from its first to its last element, and what lies between the
+ * rows is neither read nor written.  Tensors are aligned to their elements, workspaces and checkpoints to 256
+ * bytes, stats to 8.  Multiples of 8 channels with 16-byte aligned rows are the fast case.  Zero rows are
+ * allowed: nothing is read, sums are zero.  Sums are fp32, a result is rounded once to the storage type.
+ * Two calls that overlap in time need workspaces of their own.
+ * ------------------------------------------------------------------------------------------------ */
+
+/* Layer norm over the channels of [rows][c], c in [1, 16384]:
+ *   y = [add +] (x - mean) * rstd * gain + offset,   rstd = 1 / sqrt(variance + eps), variance biased.
+ *   x, add, y: of type dtype.  add: NULL, or a tensor to add to, which may be y itself (same pointer and stride): a
+ *     recycled representation is added to the trunk's input in place.
+ *   gain, offset: fp32 [c], NULL = ones, zeros.
+ *   stats: NULL, or fp32 [rows][2] that receives (mean, rstd), which the backward pass reads.
+ *   ckpt: NULL, or pe_ckpt_bytes(rows, c) bytes that receive x in 8 bits, as pe_ckpt_pack writes it, in the same pass.  */
+int pe_layernorm_fwd(pe_handle* h, long long rows, int c, int dtype,
+                     const void* x, long long ld_x, const void* add, long long ld_add,
+                     const float* gain, const float* offset, float eps,
+                     void* y, long long ld_y, float* stats, void* ckpt, void* stream);
+
+/* Backward of pe_layernorm_fwd.  With u = gain * dy and z = (x - mean) * rstd:
+ *   dx = [add +] rstd * (u - mean(u) - z * mean(u * z)),  d_gain = sum over rows of dy * z,  d_offset = sum of dy.
+ *   x_type: dtype, or PE_CKPT: x is then the checkpoint of the forward pass (ld_x is ignored) and z is formed from the
+ *     values it stands for, with the statistics of the exact ones.
+ *   dx: NULL where the input needs no gradient (recycled representations do not).  add: as in the forward pass, may be dx.
+ *   d_gain, d_offset: fp32 [c], either NULL where it is not wanted; accumulate 0: overwritten, otherwise added to.
+ *   workspace: pe_layernorm_workspace_bytes(rows, c) bytes; NULL is allowed without d_gain and d_offset.              */
+size_t pe_layernorm_workspace_bytes(long long rows, int c);
+int pe_layernorm_bwd(pe_handle* h, long long rows, int c, int dtype, int x_type,
+                     const void* x, long long ld_x, const float* stats, const float* gain,
+                     const void* dy, long long ld_dy, const void* add, long long ld_add,
+                     void* dx, long long ld_dx, float* d_gain, float* d_offset, int accumulate,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Activation checkpoint: [rows][c] in 8 bits, c in [1, 2^20].  Groups of 32 consecutive channels of a row (the last one may
+ * be shorter) share a scale 2^e, the smallest e >= -126 with max|x| <= 127 * 2^e; a code is x / 2^e rounded to the nearest
+ * integer, ties to even.  What is restored is code * 2^e, exactly, in either type; a group that holds an infinity or NaN
+ * is restored as NaN.  The error is at most 1/127 of the group's largest magnitude (or 2^-127).
+ * Layout: codes int8 [rows][c]; from the next multiple of 256 bytes on one byte e + 127 per group, [rows][ceil(c / 32)], 255
+ * for a group that was not finite.                                                                       */
+size_t pe_ckpt_bytes(long long rows, int c);
+int pe_ckpt_pack(pe_handle* h, long long rows, int c, int dtype, const void* x, long long ld_x, void* ckpt, void* stream);
+int pe_ckpt_unpack(pe_handle* h, long long rows, int c, int dtype, const void* ckpt, void* y, long long ld_y, void* stream);
+
+/* Relative position embedding by buckets.  d = pos_q[q] - pos_k[k] falls into bucket #{i : edges[i] <= d}: n_edges + 1 buckets;
+ * with `segments`, a pair of different segments (chains, documents) has a bucket of its own behind those, whatever its
+ * distance.  table: fp32 [buckets][c].
+ *   PE_RELPOS_PAIR:  out[q][k][ch] = [add +] table[bucket][ch], row q at q * ld (ld = 0: n_k * c), the pair representation;
+ *   PE_RELPOS_HEADS: out[ch][q][k] likewise, row (ch, q) at (ch * n_q + q) * ld (ld = 0: n_k), the bias of an attention.
+ * The distances clipped to +-32 of a protein's residues are edges -31, -30 .. 32.  One new position against a long sequence is n_q = 1. */
+enum { PE_RELPOS_PAIR = 0, PE_RELPOS_HEADS = 1 };
+typedef struct pe_relpos {
+  int n_q, n_k;          /* 0 .. 2^27                                                  */
+  int c;                 /* channels or heads, 1 .. 1024; n_q * n_k * c up to 10^12    */
+  int n_edges;           /* 0 .. 254                                                   */
+  int segments;          /* 0: none, 1: seg_q and seg_k are given                      */
+  int layout;            /* PE_RELPOS_PAIR | PE_RELPOS_HEADS                           */
+  int dtype;             /* PE_F32 | PE_BF16: out, add, d_out                          */
+  long long ld;          /* elements between rows q, 0 = no gaps                       */
+} pe_relpos;
+
+/* edges: HOST pointer to n_edges ascending numbers above -2^31, read during the call (and not again when a captured call is
+ * replayed).  pos_q, seg_q: int [n_q], pos_k, seg_k: int [n_k], device; any values in any order.  add: NULL, or a tensor laid out
+ * as out, which may be out itself.                                                                        */
+int pe_relpos_fwd(pe_handle* h, const pe_relpos* p, const int* edges, const int* pos_q, const int* pos_k,
+                  const int* seg_q, const int* seg_k, const float* table, const void* add, void* out, void* stream);
+/* d_table[b][ch] = sum of d_out over the pairs in bucket b, fp32 [buckets][c]; accumulate 0: overwritten, otherwise added to.
+ * The gradient of `add` is d_out itself.  workspace: pe_relpos_workspace_bytes bytes.                     */
+size_t pe_relpos_workspace_bytes(const pe_relpos* p);
+int pe_relpos_bwd(pe_handle* h, const pe_relpos* p, const int* edges, const int* pos_q, const int* pos_k,
+                  const int* seg_q, const int* seg_k, const void* d_out, float* d_table, int accumulate,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
 const char* pe_strerror(int code);
-const char* pe_last_error(pe_handle* h);   /* text of the last PE_ERR_HIP on this handle */
+const char* pe_last_error(pe_handle* h);   /* text of the last PE_ERR_HIP or refused operator call on this handle */
 
 #ifdef __cplusplus
 }

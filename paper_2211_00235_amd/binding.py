@@ -2,7 +2,8 @@
 import ctypes as C
 import os
 
-PE_F32, PE_BF16 = 0, 1
+PE_F32, PE_BF16, PE_CKPT = 0, 1, 2
+PE_RELPOS_PAIR, PE_RELPOS_HEADS = 0, 1
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libpe_mi355x.so")
 
@@ -35,6 +36,10 @@ class _CtxEntry(C.Structure):
 class _TimingEntry(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("kernel", C.c_char * 64), ("launches", C.c_int), ("total_ms", C.c_double),
                 ("flops", C.c_double), ("bytes", C.c_double)]
+
+
+class _Relpos(C.Structure):
+    _fields_ = [(k, C.c_int) for k in ("n_q", "n_k", "c", "n_edges", "segments", "layout", "dtype")] + [("ld", C.c_longlong)]
 
 
 _lib = None
@@ -76,6 +81,20 @@ def lib():
     L.pe_block_bwd.argtypes = [vp, dp, vp, vp, fp, fp, fp, vp, vp, vp, vp, fp, vp, vp, C.c_size_t, vp, vp]
     L.pe_stack_fwd_bwd.argtypes = [vp, C.c_int, dp, C.c_int, dp, vp, vp, vp, fp, fp, fp, fp, vp, vp,
                                    vp, vp, vp, vp, vp, fp, vp, C.c_size_t, vp, vp]
+    ll, rp, size = C.c_longlong, C.POINTER(_Relpos), C.c_size_t
+    L.pe_handle_device.argtypes = [vp]
+    L.pe_layernorm_fwd.argtypes = [vp, ll, C.c_int, C.c_int, vp, ll, vp, ll, fp, fp, C.c_float, vp, ll, fp, vp, vp]
+    L.pe_layernorm_workspace_bytes.argtypes = [ll, C.c_int]
+    L.pe_layernorm_workspace_bytes.restype = size
+    L.pe_layernorm_bwd.argtypes = [vp, ll, C.c_int, C.c_int, C.c_int, vp, ll, fp, fp, vp, ll, vp, ll, vp, ll, fp, fp, C.c_int, vp, size, vp]
+    L.pe_ckpt_bytes.argtypes = [ll, C.c_int]
+    L.pe_ckpt_bytes.restype = size
+    L.pe_ckpt_pack.argtypes = [vp, ll, C.c_int, C.c_int, vp, ll, vp, vp]
+    L.pe_ckpt_unpack.argtypes = [vp, ll, C.c_int, C.c_int, vp, vp, ll, vp]
+    L.pe_relpos_workspace_bytes.argtypes = [rp]
+    L.pe_relpos_workspace_bytes.restype = size
+    L.pe_relpos_fwd.argtypes = [vp, rp, vp, vp, vp, vp, vp, fp, vp, vp, vp]
+    L.pe_relpos_bwd.argtypes = [vp, rp, vp, vp, vp, vp, vp, vp, fp, C.c_int, vp, size, vp]
     L.pe_timing_collect.argtypes = [vp, C.POINTER(_TimingEntry), C.c_int]
     L.pe_strerror.argtypes = [C.c_int]
     L.pe_strerror.restype = C.c_char_p
@@ -167,6 +186,14 @@ class Handle:
         return [dict(name=e.name.decode(), kernel=e.kernel.decode(), launches=int(e.launches), total_ms=float(e.total_ms),
                      flops=float(e.flops), bytes=float(e.bytes)) for e in arr[:n]]
 
+    @property
+    def device(self):
+        """Index of the device that was current when the handle was made."""
+        d = self.__dict__.get("_device")
+        if d is None:
+            d = self._device = int(lib().pe_handle_device(self._h))
+        return d
+
     def last_error(self):
         return lib().pe_last_error(self._h).decode()
 
@@ -242,3 +269,177 @@ def stack_fwd_bwd(h, n_extra, extra, n_main, main, extra_msa_in, msa_in, pair_in
                                 _p(d_pair_in), _p(d_params), _p(workspace),
                                 workspace.numel() * workspace.element_size(), _s(stream_msa), _s(stream_pair))
     _raise(h, rc, "pe_stack_fwd_bwd")
+
+
+# ---------------------------------------------------------------------------
+# Operators around the trunk (include/pe.h says what they compute).  Tensors are torch tensors on the handle's device; a
+# tensor [..., c] counts as rows of c channels, with gaps between the rows only where it has two dimensions.
+# ---------------------------------------------------------------------------
+_DTYPES = {}
+
+
+def _dtype(t, what):
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        d = _DTYPES[t.dtype] = {"torch.float32": PE_F32, "torch.bfloat16": PE_BF16, "torch.uint8": PE_CKPT,
+                                "torch.int32": "int32"}.get(str(t.dtype), "other")
+    return d
+
+
+def _on(h, t, what):
+    if not t.is_cuda or t.get_device() != h.device:
+        raise PEError("%s: not on the handle's device" % what)
+
+
+def _rows(h, t, what, like=None):
+    """(type, rows, c, row stride) of a tensor of activations; `like`: what another one has to agree with."""
+    _on(h, t, what)
+    d, shape = _dtype(t, what), t.shape
+    if d not in (PE_F32, PE_BF16) or not shape:
+        raise PEError("%s: a float32 or bfloat16 tensor [..., c] is wanted" % what)
+    c = shape[-1]
+    if len(shape) == 2 and (c == 1 or t.stride(1) == 1):
+        rows, ld = shape[0], (t.stride(0) if shape[0] > 1 else c)
+    elif t.is_contiguous():
+        rows, ld = (t.numel() // c if c else 0), c
+    else:
+        raise PEError("%s: channels have to be neighbours in memory, rows of a tensor with more than two dimensions too" % what)
+    if like is not None and like != (d, rows, c):
+        raise PEError("%s: shape or type differs" % what)
+    return d, rows, c, ld
+
+
+def _vec(h, t, n, what, dtype=PE_F32):
+    """Device pointer of a contiguous tensor of n elements (None: NULL)."""
+    if t is None:
+        return None
+    _on(h, t, what)
+    if _dtype(t, what) != dtype or t.numel() != n or not t.is_contiguous():
+        raise PEError("%s: a contiguous tensor of %d elements is wanted" % (what, n))
+    return t.data_ptr()
+
+
+def _bytes(h, t, n, what):
+    if t is None:
+        return None
+    _on(h, t, what)
+    if not t.is_contiguous() or t.numel() * t.element_size() < n:
+        raise PEError("%s: %d contiguous bytes are wanted" % (what, n))
+    return t.data_ptr()
+
+
+def _op(h, rc, what):
+    if rc:
+        raise PEError("%s: %s %s" % (what, strerror(rc), h.last_error()))
+
+
+def layernorm_fwd(h, x, gain, offset, y, eps=1e-5, add=None, stats=None, ckpt=None, stream=None):
+    """y = [add +] LayerNorm(x); stats float32 [rows, 2]; ckpt: uint8 tensor of ckpt_bytes(rows, c) bytes that receives x."""
+    d, rows, c, ld = _rows(h, x, "x")
+    like = (d, rows, c)
+    ldy = _rows(h, y, "y", like)[3]
+    lda = _rows(h, add, "add", like)[3] if add is not None else 0
+    _op(h, lib().pe_layernorm_fwd(
+        h._h, rows, c, d, x.data_ptr(), ld, None if add is None else add.data_ptr(), lda, _vec(h, gain, c, "gain"),
+        _vec(h, offset, c, "offset"), eps, y.data_ptr(), ldy, _vec(h, stats, 2 * rows, "stats"),
+        None if ckpt is None else _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), _s(stream)), "pe_layernorm_fwd")
+
+
+def layernorm_workspace_bytes(rows, c):
+    return int(lib().pe_layernorm_workspace_bytes(rows, c))
+
+
+def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=None, accumulate=False, stream=None):
+    """Gradients of layernorm_fwd.  x: its input, or the uint8 checkpoint that it wrote.  dx, d_gain, d_offset: None where
+    not wanted."""
+    d, rows, c, ldy = _rows(h, dy, "dy")
+    like = (d, rows, c)
+    kept = _dtype(x, "x") == PE_CKPT
+    if kept:
+        px, ldx = _bytes(h, x, ckpt_bytes(rows, c), "x"), 0
+    else:
+        ldx, px = _rows(h, x, "x", like)[3], x.data_ptr()
+    lda = _rows(h, add, "add", like)[3] if add is not None else 0
+    ldd = _rows(h, dx, "dx", like)[3] if dx is not None else 0
+    ws = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _op(h, lib().pe_layernorm_bwd(
+        h._h, rows, c, d, PE_CKPT if kept else d, px, ldx, _vec(h, stats, 2 * rows, "stats"), _vec(h, gain, c, "gain"),
+        dy.data_ptr(), ldy, None if add is None else add.data_ptr(), lda, None if dx is None else dx.data_ptr(), ldd,
+        _vec(h, d_gain, c, "d_gain"), _vec(h, d_offset, c, "d_offset"), int(accumulate), _bytes(h, workspace, 0, "workspace"),
+        ws, _s(stream)), "pe_layernorm_bwd")
+
+
+def ckpt_bytes(rows, c):
+    return int(lib().pe_ckpt_bytes(rows, c))
+
+
+def ckpt_pack(h, x, ckpt, stream=None):
+    """x [..., c] in 8 bits into the uint8 tensor ckpt (ckpt_bytes(rows, c) bytes)."""
+    d, rows, c, ld = _rows(h, x, "x")
+    _op(h, lib().pe_ckpt_pack(h._h, rows, c, d, x.data_ptr(), ld, _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), _s(stream)),
+        "pe_ckpt_pack")
+
+
+def ckpt_unpack(h, ckpt, y, stream=None):
+    d, rows, c, ld = _rows(h, y, "y")
+    _op(h, lib().pe_ckpt_unpack(h._h, rows, c, d, _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), y.data_ptr(), ld, _s(stream)),
+        "pe_ckpt_unpack")
+
+
+_LAYOUTS = {"pair": PE_RELPOS_PAIR, "heads": PE_RELPOS_HEADS}
+
+
+def _relpos(h, pos_q, pos_k, edges, t, seg_q, seg_k, layout, what):
+    """Description of a call from its tensors: t is out or d_out, [q, k, c] or [c, q, k] with unit stride along its last axis
+    ("pair": the last two axes without gaps)."""
+    _on(h, t, what)
+    if layout not in _LAYOUTS:
+        raise PEError("layout: 'pair' or 'heads'")
+    if (seg_q is None) != (seg_k is None):
+        raise PEError("segments: seg_q and seg_k belong together")
+    if edges.is_cuda or _dtype(edges, "edges") != "int32" or not edges.is_contiguous():
+        raise PEError("edges: a contiguous int32 tensor in host memory is wanted")
+    n_q, n_k = pos_q.numel(), pos_k.numel()
+    pair, d = layout == "pair", _dtype(t, what)
+    if d not in (PE_F32, PE_BF16) or t.dim() != 3:
+        raise PEError("%s: a float32 or bfloat16 tensor of three dimensions is wanted" % what)
+    s, st = t.shape, t.stride()
+    c = s[2] if pair else s[0]
+    if tuple(s) != ((n_q, n_k, c) if pair else (c, n_q, n_k)):
+        raise PEError("%s: shape differs from the positions'" % what)
+    ld = 0
+    if not t.is_contiguous():
+        ok = st[2] == 1 and (st[1] == c if pair else st[0] == n_q * st[1])
+        ld = st[0] if pair else st[1]
+        if not ok or ld < (n_k * c if pair else n_k):
+            raise PEError("%s: gaps are allowed between rows q only" % what)
+    p = _Relpos(n_q, n_k, c, edges.numel(), 0 if seg_q is None else 1, _LAYOUTS[layout], d, ld)
+    ptr = (edges.data_ptr() if edges.numel() else None, _vec(h, pos_q, n_q, "pos_q", "int32"), _vec(h, pos_k, n_k, "pos_k", "int32"),
+           _vec(h, seg_q, n_q, "seg_q", "int32"), _vec(h, seg_k, n_k, "seg_k", "int32"))
+    return p, ptr, (edges.numel() + (1 if seg_q is None else 2)) * c
+
+
+def relpos_fwd(h, pos_q, pos_k, edges, table, out, seg_q=None, seg_k=None, add=None, layout="pair", stream=None):
+    """out = [add +] table[bucket(pos_q - pos_k)]; edges: int32 tensor in host memory, table float32 [buckets, c]."""
+    p, ptr, n = _relpos(h, pos_q, pos_k, edges, out, seg_q, seg_k, layout, "out")
+    if add is not None:
+        _on(h, add, "add")
+        if add.dtype != out.dtype or add.shape != out.shape or add.stride() != out.stride():
+            raise PEError("add: laid out as out is wanted")
+    _op(h, lib().pe_relpos_fwd(h._h, C.byref(p), *ptr, _vec(h, table, n, "table"), None if add is None else add.data_ptr(),
+                               out.data_ptr(), _s(stream)), "pe_relpos_fwd")
+
+
+def relpos_workspace_bytes(n_q, n_k, c, buckets, layout="pair"):
+    """Bytes for relpos_bwd; buckets: rows of the table."""
+    segments = int(buckets > 1)
+    p = _Relpos(n_q, n_k, c, buckets - 1 - segments, segments, _LAYOUTS[layout], PE_F32, 0)
+    return int(lib().pe_relpos_workspace_bytes(C.byref(p)))
+
+
+def relpos_bwd(h, pos_q, pos_k, edges, d_out, d_table, workspace, seg_q=None, seg_k=None, layout="pair", accumulate=False, stream=None):
+    """d_table [buckets, c] = sum of d_out over the pairs of each bucket."""
+    p, ptr, n = _relpos(h, pos_q, pos_k, edges, d_out, seg_q, seg_k, layout, "d_out")
+    _op(h, lib().pe_relpos_bwd(h._h, C.byref(p), *ptr, d_out.data_ptr(), _vec(h, d_table, n, "d_table"), int(accumulate),
+                               _bytes(h, workspace, 0, "workspace"), workspace.numel() * workspace.element_size(), _s(stream)),
+        "pe_relpos_bwd")

@@ -1,11 +1,12 @@
 """Build the HIP library in-tree for gfx950 (hipcc cross-compiles without a GPU)."""
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpe_mi355x.so")
-SOURCES = ["pe_block.hip"]
+SOURCES = ["pe_block.hip", "pe_ops.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-mfma-vgpr-form",      # MFMA accumulators in VGPRs: no AGPR<->VGPR copies around the softmax
@@ -13,19 +14,28 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 
 
 def build(verbose=False):
+    """Compiles the sources side by side and links them."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode:
-        lines = [l for l in (res.stdout + res.stderr).splitlines() if "packed-fp32-ops" not in l]
-        print("\n".join(lines))
-    if res.returncode:
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        flags = [f for f in FLAGS if f != "-shared"]
+        procs = [subprocess.Popen([hipcc] + flags + ["-c", os.path.join(CSRC, s), "-o", o], stdout=subprocess.PIPE,
+                                  stderr=subprocess.STDOUT, text=True) for s, o in zip(SOURCES, objs)]
+        said = [p.communicate()[0] for p in procs]
+        failed = any(p.returncode for p in procs)
+        if not failed:
+            res = subprocess.run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared"] + objs + ["-o", LIB], capture_output=True, text=True)
+            said.append(res.stdout + res.stderr)
+            failed = res.returncode != 0
+    if verbose or failed:
+        print("\n".join(l for l in "\n".join(said).splitlines() if "packed-fp32-ops" not in l))
+    if failed:
         raise RuntimeError("hipcc failed building %s" % LIB)
     return LIB
 
 
-def build_host_check(out, verbose=False):
-    """Host-only exercise of the C ABI (tests/host_checks/abi_host_check.cpp) linked with the library's source, the
+def build_host_check(out, verbose=False, program="abi_host_check.cpp", sources=SOURCES):
+    """Host-only exercise of the C ABI (a program of tests/host_checks) linked with the library's sources, the
     HOST code instrumented with AddressSanitizer and UndefinedBehaviorSanitizer (the device code is compiled as
     usual and never run: the program calls nothing that needs a GPU)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -33,8 +43,8 @@ def build_host_check(out, verbose=False):
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=undefined"]
     flags = [f for f in FLAGS if f not in ("-shared", "-fPIC", "-O3")] + ["-O1", "-g"]
-    cmd = ([hipcc] + flags + san + [os.path.join(CSRC, s) for s in SOURCES] +
-           [os.path.join(root, "tests", "host_checks", "abi_host_check.cpp"), "-o", out])
+    cmd = ([hipcc] + flags + san + [os.path.join(CSRC, s) for s in sources] +
+           [os.path.join(root, "tests", "host_checks", program), "-o", out])
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode:
         print("\n".join(l for l in (res.stdout + res.stderr).splitlines() if "packed-fp32-ops" not in l))

@@ -17,6 +17,7 @@
 #include "pe_deep.h"
 #include "pe_gcol.h"
 #include "pe_gemm.h"
+#include "pe_handle.h"
 #include "pe_layout.h"
 #include "pe_pipe.h"
 #include "pe_rows.h"
@@ -33,27 +34,6 @@ static __device__ __align__(256) unsigned char scratch[PE_STATIC_SCRATCH_BYTES];
 #define PE_MAX_DEVICES 64
 static void* g_scratch_ptr[PE_MAX_DEVICES];
 static std::mutex g_scratch_mutex;
-
-struct ProfRec { const char* label; std::string kern; double flops, bytes; hipEvent_t e0, e1; };
-struct pe_handle {
-  int device;                       // device that was current in pe_create
-  void* static_scratch;             // that device's copy of `scratch`
-  hipEvent_t ev[6];
-  int branches;
-  int sync_debug;
-  int timing;                       // PE_OPT_KERNEL_TIMING
-  int side_streams;                 // PE_OPT_SIDE_STREAMS
-  int stack_keep;                   // PE_OPT_STACK_KEEP_CTX
-  int stack_overlap;                // PE_OPT_STACK_OVERLAP
-  hipStream_t side[2];              // side stream of the MSA branch / of the pair branch
-  hipEvent_t side_ev[32];           // ring of fork/join events
-  int side_ev_next;
-  hipStream_t pair;                 // the pair branch's stream of calls with one stream (pair_stream); null: there is none
-  bool pair_forked;                 // the call that is running has forked it from the caller's stream
-  std::vector<ProfRec> recs;        // one per timed launch since the last collect
-  std::vector<hipEvent_t> ev_pool;  // reusable timing events
-  std::string last_error;
-};
 
 // ---------------------------------------------------------------------------
 // bump allocators
@@ -2161,21 +2141,6 @@ static int stack_impl(pe_handle* h, int n_extra, const pe_dims* ex, int n_main, 
 // ---------------------------------------------------------------------------
 // C ABI
 // ---------------------------------------------------------------------------
-static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const char* x = (const char*)a; const char* y = (const char*)b;
-  return x < y + nb && y < x + na;
-}
-// a buffer of a call: written = the call writes it (outputs, ctx of the forward, workspace)
-struct Region { const void* p; size_t n; bool written; };
-// true when two buffers overlap of which at least one is written (null and empty buffers are skipped)
-static bool any_alias(const Region* r, int n) {
-  for (int i = 0; i < n; i++)
-    for (int j = i + 1; j < n; j++)
-      if ((r[i].written || r[j].written) && r[i].p && r[j].p && r[i].n && r[j].n && overlap(r[i].p, r[i].n, r[j].p, r[j].n))
-        return true;
-  return false;
-}
-
 // Streams of the pair branch (pair_stream).  A handle takes one for itself when it is created and gives it back when it is destroyed, with what is
 // queued on it, so that neither waits for the device and a compute call creates nothing (a stream costs 120 us, almost half of a
 // short protein's forward pass; waiting in pe_destroy cost 50).  Up to PAIR_KEPT idle ones are kept per device until the process ends.

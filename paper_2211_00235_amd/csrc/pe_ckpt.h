@@ -1,0 +1,106 @@
+// Activation checkpoints in 8 bits.
+//
+// Groups of 32 consecutive channels of a row share a scale 2^e: the smallest e >= -126 with max|x| <= 127 2^e.  A code is
+// rint(x 2^-e), the value it stands for code 2^e.  A power of two makes every step but that one rounding exact (scaling,
+// restoring, and the restored value in bf16: 7 bits of magnitude), so packing what was restored gives the same codes,
+// and the result does not depend on how a division rounds.  The error is at most 2^(e-1), between 1/254 and 1/127 of the group's
+// largest magnitude.  A group that holds an infinity or NaN is restored as NaN throughout: the loss stays visible.
+//
+// Layout of a checkpoint of [rows][c]: int8 codes [rows][c], then, at the next multiple of 256 bytes, one byte e + 127 per
+// group, [rows][ceil(c / 32)]; 255 marks a group that was not finite.
+#pragma once
+#include "pe_lanes.h"
+
+constexpr int CK_GROUP = 32;
+
+// largest magnitude's bits (sign cleared) -> the group's scale byte
+PE_DEV uint32_t ck_scale_byte(uint32_t m) {
+  const int sb = (int)(m >> 23) - 6 + ((m & 0x7fffffu) > 0x7e0000u ? 1 : 0);     // 64 <= max|x| 2^-e <= 127; above 127/64 of a power of two: the next e
+  return m >= 0x7f800000u ? 255u : (uint32_t)max(sb, 1);
+}
+PE_DEV float ck_inverse(uint32_t sb) { return __uint_as_float((254u - sb) << 23); }    // 2^-e, sb 1..249
+PE_DEV float ck_scale(uint32_t sb) { return sb == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(sb << 23); }
+PE_DEV int ck_code(float x, float inv) { return (int)rintf(x * inv); }
+
+template <int V> struct Codes;       // V consecutive codes
+template <> struct Codes<8> {
+  uint2 v;
+  PE_DEV int get(int i) const { return (int)(int8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3))); }
+  PE_DEV void clear() { v.x = v.y = 0; }
+  PE_DEV void put(int i, int c) { (i < 4 ? v.x : v.y) |= ((uint32_t)c & 255u) << (8 * (i & 3)); }
+};
+template <> struct Codes<2> {
+  uint16_t v;
+  PE_DEV int get(int i) const { return (int)(int8_t)(v >> (8 * i)); }
+  PE_DEV void clear() { v = 0; }
+  PE_DEV void put(int i, int c) { v |= (uint16_t)(((uint32_t)c & 255u) << (8 * i)); }
+};
+template <> struct Codes<1> {
+  int8_t v;
+  PE_DEV int get(int) const { return (int)v; }
+  PE_DEV void clear() { v = 0; }
+  PE_DEV void put(int, int c) { v = (int8_t)c; }
+};
+
+// V elements of a group's 32 / V lanes -> the scale byte of the group (in all of its lanes) and this lane's codes.  Elements
+// behind the last channel have to be zero.
+template <int V> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>& codes) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < V; i++) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);    // as integers NaN is above infinity above every number
+  const uint32_t sb = ck_scale_byte(lanes_umax<CK_GROUP / V>(m));
+  const float inv = ck_inverse(sb == 255u ? 127u : sb);
+  codes.clear();
+#pragma unroll
+  for (int i = 0; i < V; i++) codes.put(i, sb == 255u ? 0 : ck_code(x[i], inv));
+  return sb;
+}
+
+// One item = V channels of a row; a row has `per_row` items, a multiple of a group's 32 / V, of which those from `n_vec` on hold no
+// channel.  A workgroup takes U runs of 256 consecutive items, all of its loads in flight at once.  HBM-bound.
+template <typename T, int V, int U, bool PACK>
+__global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int8_t* codes, uint8_t* scales, T* y, long long rows,
+                                                   int c, int per_row) {
+  constexpr int LG = CK_GROUP / V;
+  const int groups = per_row / LG, n_vec = c / V;
+  const long long first = (long long)blockIdx.x * (256 * U);
+  const long long row0 = first / per_row;
+  const uint32_t rem = (uint32_t)(first - row0 * per_row) + threadIdx.x;
+  long long row[U];
+  int vec[U];
+  bool in[U];
+  Raw<T, V> v[U];
+  Codes<V> cd[U];
+  uint32_t sb[U];
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    const uint32_t off = rem + 256u * u, dr = off / (uint32_t)per_row;
+    row[u] = row0 + dr;
+    vec[u] = (int)(off - dr * (uint32_t)per_row);
+    in[u] = row[u] < rows && vec[u] < n_vec;
+    if constexpr (PACK) {
+      v[u] = in[u] ? raw_load<T, V>(x + row[u] * ld + (long long)vec[u] * V) : raw_zero<T, V>();
+    } else if (in[u]) {
+      cd[u] = *reinterpret_cast<const Codes<V>*>(codes + row[u] * c + (long long)vec[u] * V);
+      sb[u] = scales[row[u] * groups + vec[u] / LG];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    if constexpr (PACK) {
+      float f[V];
+#pragma unroll
+      for (int i = 0; i < V; i++) f[i] = v[u].get(i);
+      const uint32_t s = ck_encode<V>(f, cd[u]);
+      if (in[u]) {
+        *reinterpret_cast<Codes<V>*>(codes + row[u] * c + (long long)vec[u] * V) = cd[u];
+        if (vec[u] % LG == 0) scales[row[u] * groups + vec[u] / LG] = (uint8_t)s;
+      }
+    } else if (in[u]) {
+      const float s = ck_scale(sb[u]);
+#pragma unroll
+      for (int i = 0; i < V; i++) v[u].set(i, (float)cd[u].get(i) * s);
+      raw_store<T, V>(y + row[u] * ld + (long long)vec[u] * V, v[u]);
+    }
+  }
+}

@@ -1,0 +1,74 @@
+// Sums and maxima over groups of consecutive lanes on the vector unit (DPP and lane swaps; __shfl_xor goes through LDS), and
+// vectors of V elements in fp32.
+#pragma once
+#include "pe_common.h"
+
+template <int CTRL> PE_DEV uint32_t dpp_u(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+template <int CTRL> PE_DEV float dpp_f(float v) { return __uint_as_float(dpp_u<CTRL>(__float_as_uint(v))); }
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
+
+// Sum over the L consecutive lanes that a lane belongs to (L a power of two, at most 64); every lane gets the same bits.
+// Quads are level after two steps, so the mirrored lane of 8, then of 16, holds the other half's sum.
+template <int L> PE_DEV float lanes_sum(float v) {
+  if constexpr (L >= 2) v += dpp_f<DPP_XOR1>(v);
+  if constexpr (L >= 4) v += dpp_f<DPP_XOR2>(v);
+  if constexpr (L >= 8) v += dpp_f<DPP_HALF_MIRROR>(v);
+  if constexpr (L >= 16) v += dpp_f<DPP_MIRROR>(v);
+  if constexpr (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (L >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
+// Sum over the lanes that are a multiple of L apart (the lanes of a wave that hold the same columns)
+template <int L> PE_DEV float strided_sum(float v) {
+  static_assert(L >= 4, "quads stay apart");
+  if constexpr (L <= 4) v += __shfl_xor(v, 4, 64);
+  if constexpr (L <= 8) v += __shfl_xor(v, 8, 64);
+  if constexpr (L <= 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (L <= 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
+template <int L> PE_DEV uint32_t lanes_umax(uint32_t v) {
+  static_assert(L <= 32, "groups of at most 32 lanes");
+  if constexpr (L >= 2) v = max(v, dpp_u<DPP_XOR1>(v));
+  if constexpr (L >= 4) v = max(v, dpp_u<DPP_XOR2>(v));
+  if constexpr (L >= 8) v = max(v, dpp_u<DPP_HALF_MIRROR>(v));
+  if constexpr (L >= 16) v = max(v, dpp_u<DPP_MIRROR>(v));
+  if constexpr (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)r[0], (uint32_t)r[1]);
+  }
+  return v;
+}
+
+// V consecutive elements as they lie in memory: V = 8 needs 16-byte aligned addresses, V = 2 twice the element's size
+template <typename T, int V> struct Raw;
+template <> struct Raw<bf16, 8> { bf16x8 v; PE_DEV float get(int i) const { return (float)v[i]; } PE_DEV void set(int i, float f) { v[i] = (bf16)f; } };
+template <> struct Raw<bf16, 2> { bf16x2 v; PE_DEV float get(int i) const { return (float)v[i]; } PE_DEV void set(int i, float f) { v[i] = (bf16)f; } };
+template <> struct Raw<bf16, 1> { bf16 v; PE_DEV float get(int) const { return (float)v; } PE_DEV void set(int, float f) { v = (bf16)f; } };
+template <> struct Raw<float, 8> {
+  f32x4 v[2];
+  PE_DEV float get(int i) const { return v[i >> 2][i & 3]; }
+  PE_DEV void set(int i, float f) { v[i >> 2][i & 3] = f; }
+};
+template <> struct Raw<float, 2> { f32x2 v; PE_DEV float get(int i) const { return v[i]; } PE_DEV void set(int i, float f) { v[i] = f; } };
+template <> struct Raw<float, 1> { float v; PE_DEV float get(int) const { return v; } PE_DEV void set(int, float f) { v = f; } };
+template <typename T, int V> PE_DEV Raw<T, V> raw_load(const T* p) { return *reinterpret_cast<const Raw<T, V>*>(p); }
+template <typename T, int V> PE_DEV void raw_store(T* p, const Raw<T, V>& r) { *reinterpret_cast<Raw<T, V>*>(p) = r; }
+template <typename T, int V> PE_DEV Raw<T, V> raw_zero() {
+  Raw<T, V> r;
+#pragma unroll
+  for (int i = 0; i < V; i++) r.set(i, 0.0f);
+  return r;
+}

@@ -1,0 +1,312 @@
+// Layer norm as an operator of its own: forward and backward over [rows][c] with row strides.
+//
+//   y  = [add +] (x - mean) rstd gain + offset                                    mean, rstd: of the row, variance in two passes
+//   dx = [add +] rstd (u - mean(u) - z mean(u z)),  u = gain dy,  z = (x - mean) rstd
+//   d_gain = sum over rows of dy z,  d_offset = sum over rows of dy
+//
+// HBM-bound: 8 vector operations per element forward, 15 backward, against 4 to 8 bytes.  A row lies in the registers of L
+// lanes (NV vectors of V elements each), so that it is read once: L = 4..64 lanes, several rows per wave, up to 2048 channels,
+// whole workgroups above.  Statistics and sums are fp32; a result is rounded once, to the storage type.  A lane keeps its columns'
+// d_gain and d_offset in registers over all of its rows; workgroups write one fp32 partial each, and columns_sum_kernel adds
+// them in a fixed order.
+#pragma once
+#include "pe_ckpt.h"
+
+struct LnArgs {
+  const void* x; long long ld_x;          // x, or null where codes / scales hold it in 8 bits
+  const int8_t* codes; const uint8_t* scales;
+  const void* add; long long ld_add;
+  const void* dy; long long ld_dy;
+  void* out; long long ld_out;            // y, or dx (null: not wanted)
+  int8_t* k_codes; uint8_t* k_scales;     // forward: x in 8 bits (null: not wanted)
+  const float* gain; const float* offset; // null: 1, 0
+  float* stats;
+  const float* stats_in;
+  float* part;                            // backward: [workgroups][2][c] (null: not wanted)
+  long long rows;
+  int c;
+  float eps;
+};
+
+// Sum over the L lanes of a row; above 64 lanes the waves of the workgroup exchange theirs through `red`.  A row uses two
+// slots of `red` and the next row the other two, so one barrier per sum is enough.
+template <int L> PE_DEV float row_sum(float v, float* red) {
+  v = lanes_sum<(L < 64 ? L : 64)>(v);
+  if constexpr (L > 64) {
+    constexpr int W = L / 64;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; w++) v += red[w];
+  }
+  return v;
+}
+
+// Workgroup shape of a row of L lanes: rows side by side
+template <int L> struct LnShape {
+  static constexpr int THREADS = L > 256 ? L : 256;
+  static constexpr int ROWS = THREADS / L;
+};
+
+template <typename T, int V, int L, int NV>
+__global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const LnArgs a) {
+  constexpr int ROWS = LnShape<L>::ROWS, LG = CK_GROUP / V;
+  __shared__ float red[4][16];
+  const int li = threadIdx.x % L;                        // this lane's place in its row
+  const int c = a.c, n_vec = c / V;
+  const float inv_c = 1.0f / (float)c;
+  bool in[NV];
+#pragma unroll
+  for (int n = 0; n < NV; n++) in[n] = n * L + li < n_vec;
+  constexpr bool HELD = NV * V <= 8;      // gain and offset stay in registers, and the next row is requested ahead
+  auto gain_of = [&](int n, int i) { return in[n] && a.gain ? a.gain[(n * L + li) * V + i] : 1.0f; };
+  auto offs_of = [&](int n, int i) { return in[n] && a.offset ? a.offset[(n * L + li) * V + i] : 0.0f; };
+  float gain[HELD ? NV : 1][V], offs[HELD ? NV : 1][V];
+  if constexpr (HELD) {
+#pragma unroll
+    for (int n = 0; n < NV; n++)
+#pragma unroll
+      for (int i = 0; i < V; i++) { gain[n][i] = gain_of(n, i); offs[n][i] = offs_of(n, i); }
+  }
+  const T* x = (const T*)a.x;
+  const T* add = (const T*)a.add;
+  T* y = (T*)a.out;
+  long long row = (long long)blockIdx.x * ROWS + threadIdx.x / L;
+  const long long step = (long long)gridDim.x * ROWS;
+  Raw<T, V> next[NV];
+  auto fetch = [&](long long r) {
+#pragma unroll
+    for (int n = 0; n < NV; n++)
+      next[n] = in[n] && r < a.rows ? raw_load<T, V>(x + r * a.ld_x + (n * L + li) * V) : raw_zero<T, V>();
+  };
+  if constexpr (HELD) fetch(row);
+  int slot = 0;
+  for (; row < a.rows; row += step, slot ^= 2) {
+    Raw<T, V> v[NV], ad[NV];
+    if constexpr (!HELD) fetch(row);
+#pragma unroll
+    for (int n = 0; n < NV; n++) v[n] = next[n];
+    if (add) {
+#pragma unroll
+      for (int n = 0; n < NV; n++)
+        if (in[n]) ad[n] = raw_load<T, V>(add + row * a.ld_add + (n * L + li) * V);
+    }
+    if constexpr (HELD) fetch(row + step);
+    float s = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NV; n++)
+#pragma unroll
+      for (int i = 0; i < V; i++) s += v[n].get(i);
+    const float mean = row_sum<L>(s, red[slot]) * inv_c;
+    float q = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NV; n++)
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        const float t = in[n] ? v[n].get(i) - mean : 0.0f;
+        q += t * t;
+      }
+    const float rstd = rsqrtf(row_sum<L>(q, red[slot + 1]) * inv_c + a.eps);
+    if (a.stats && li == 0) *reinterpret_cast<f32x2*>(a.stats + 2 * row) = f32x2{mean, rstd};
+#pragma unroll
+    for (int n = 0; n < NV; n++) {
+      Raw<T, V> o;
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        float g, b;
+        if constexpr (HELD) { g = gain[n][i]; b = offs[n][i]; } else { g = gain_of(n, i); b = offs_of(n, i); }
+        float f = (v[n].get(i) - mean) * rstd * g + b;
+        if (add) f += ad[n].get(i);
+        o.set(i, f);
+      }
+      if (in[n]) raw_store<T, V>(y + row * a.ld_out + (n * L + li) * V, o);
+      if constexpr (L >= LG) {
+        if (a.k_codes) {
+          float f[V];
+#pragma unroll
+          for (int i = 0; i < V; i++) f[i] = v[n].get(i);
+          Codes<V> cd;
+          const uint32_t sb = ck_encode<V>(f, cd);
+          if (in[n]) {
+            const int vec = n * L + li;
+            *reinterpret_cast<Codes<V>*>(a.k_codes + row * c + vec * V) = cd;
+            if (vec % LG == 0) a.k_scales[row * ((c + CK_GROUP - 1) / CK_GROUP) + vec / LG] = (uint8_t)sb;
+          }
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int V, int L, int NV, bool KEPT>
+__global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const LnArgs a) {
+  constexpr int ROWS = LnShape<L>::ROWS, LG = CK_GROUP / V, W = LnShape<L>::THREADS / 64;
+  __shared__ float red[4][16];
+  const int li = threadIdx.x % L;
+  const int c = a.c, n_vec = c / V, groups = (c + CK_GROUP - 1) / CK_GROUP;
+  const float inv_c = 1.0f / (float)c;
+  bool in[NV];
+#pragma unroll
+  for (int n = 0; n < NV; n++) in[n] = n * L + li < n_vec;
+  constexpr bool HELD = NV * V <= 8;
+  auto gain_of = [&](int n, int i) { return in[n] && a.gain ? a.gain[(n * L + li) * V + i] : 1.0f; };
+  float gain[HELD ? NV : 1][V], dg[NV][V], db[NV][V];
+#pragma unroll
+  for (int n = 0; n < NV; n++)
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+      if constexpr (HELD) gain[n][i] = gain_of(n, i);
+      dg[n][i] = db[n][i] = 0.0f;
+    }
+  auto u_of = [&](int n, int i, float d) {
+    if constexpr (HELD) return d * gain[n][i]; else return d * gain_of(n, i);
+  };
+  const T* x = (const T*)a.x;
+  const T* dy = (const T*)a.dy;
+  const T* add = (const T*)a.add;
+  T* dx = (T*)a.out;
+  long long row = (long long)blockIdx.x * ROWS + threadIdx.x / L;
+  const long long step = (long long)gridDim.x * ROWS;
+  Raw<T, V> nx[NV], ny[NV];
+  Codes<V> nc[NV];
+  uint32_t nsb[NV];
+  f32x2 nst;
+  auto fetch = [&](long long r) {
+    const bool live = r < a.rows;
+    nst = live ? *reinterpret_cast<const f32x2*>(a.stats_in + 2 * r) : f32x2{0.0f, 0.0f};
+#pragma unroll
+    for (int n = 0; n < NV; n++) {
+      const int vec = n * L + li;
+      const bool on = in[n] && live;
+      ny[n] = on ? raw_load<T, V>(dy + r * a.ld_dy + vec * V) : raw_zero<T, V>();
+      if constexpr (KEPT) {
+        nc[n].clear();
+        nsb[n] = 0;
+        if (on) {
+          nc[n] = *reinterpret_cast<const Codes<V>*>(a.codes + r * c + vec * V);
+          nsb[n] = a.scales[r * groups + vec / LG];
+        }
+      } else {
+        nx[n] = on ? raw_load<T, V>(x + r * a.ld_x + vec * V) : raw_zero<T, V>();
+      }
+    }
+  };
+  if constexpr (HELD) fetch(row);
+  int slot = 0;
+  for (; row < a.rows; row += step, slot ^= 2) {
+    Raw<T, V> y[NV], ad[NV], xv[NV];
+    Codes<V> cd[NV];
+    float sc[NV];
+    if constexpr (!HELD) fetch(row);
+    const float mean = nst[0], rstd = nst[1];
+#pragma unroll
+    for (int n = 0; n < NV; n++) {
+      y[n] = ny[n];
+      if constexpr (KEPT) { cd[n] = nc[n]; sc[n] = ck_scale(nsb[n]); } else xv[n] = nx[n];
+    }
+    if (add && dx) {
+#pragma unroll
+      for (int n = 0; n < NV; n++)
+        if (in[n]) ad[n] = raw_load<T, V>(add + row * a.ld_add + (n * L + li) * V);
+    }
+    if constexpr (HELD) fetch(row + step);
+    auto z_of = [&](int n, int i) {
+      float f;
+      if constexpr (KEPT) f = (float)cd[n].get(i) * sc[n]; else f = xv[n].get(i);
+      return (f - mean) * rstd;
+    };
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int n = 0; n < NV; n++)
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        const float d = y[n].get(i), z = in[n] ? z_of(n, i) : 0.0f, u = u_of(n, i, d);
+        dg[n][i] += d * z;
+        db[n][i] += d;
+        s1 += u;
+        s2 += u * z;
+      }
+    if (dx) {
+      const float m1 = row_sum<L>(s1, red[slot]) * inv_c, m2 = row_sum<L>(s2, red[slot + 1]) * inv_c;
+#pragma unroll
+      for (int n = 0; n < NV; n++) {
+        Raw<T, V> o;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+          float f = rstd * (u_of(n, i, y[n].get(i)) - m1 - z_of(n, i) * m2);
+          if (add) f += ad[n].get(i);
+          o.set(i, f);
+        }
+        if (in[n]) raw_store<T, V>(dx + row * a.ld_out + (n * L + li) * V, o);
+      }
+    }
+  }
+  if (!a.part) return;
+  float* part = a.part + (long long)blockIdx.x * 2 * c;
+  if constexpr (L <= 64) {     // the lanes of a wave that hold the same columns, then the waves
+    __shared__ float cols[2][W][L][V];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int n = 0; n < NV; n++) {
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        if constexpr (L < 64) { dg[n][i] = strided_sum<L>(dg[n][i]); db[n][i] = strided_sum<L>(db[n][i]); }
+        if (lane < L) { cols[0][wave][lane][i] = dg[n][i]; cols[1][wave][lane][i] = db[n][i]; }
+      }
+      __syncthreads();
+      for (int k = threadIdx.x; k < 2 * L * V; k += LnShape<L>::THREADS) {
+        const int t = k / (L * V), e = k % (L * V), ch = n * L * V + e;
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; w++) s += (&cols[t][w][0][0])[e];
+        if (ch < c) part[t * c + ch] = s;
+      }
+      __syncthreads();
+    }
+  } else {                     // every column is one lane's
+#pragma unroll
+    for (int n = 0; n < NV; n++)
+      if (in[n])
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+          const int ch = (n * L + li) * V + i;
+          part[ch] = dg[n][i];
+          part[c + ch] = db[n][i];
+        }
+  }
+}
+
+// out[col] (+)= sum over p of part[p][col], in a fixed order: a workgroup has 16 columns (64 bytes of a partial) and 64 lanes per
+// column, which add every 64th partial each; then a tree.  Columns from `split` on go to out1.  The loads of a thread do not
+// wait for one another: with a thread per column 1024 partials took longer than the pass that wrote them.
+__global__ __launch_bounds__(1024) void columns_sum_kernel(const float* part, int n_part, int cols, float* out0, float* out1, int split,
+                                                           int accumulate) {
+  __shared__ float sums[64][17];
+  const int cl = threadIdx.x & 15, p0 = threadIdx.x >> 4, col = blockIdx.x * 16 + cl;
+  float s = 0.0f;
+  if (col < cols) {
+    int p = p0;
+    for (; p + 192 < n_part; p += 256) {
+      const float* q = part + (long long)p * cols + col;
+      const long long st = 64LL * cols;
+      const float v0 = q[0], v1 = q[st], v2 = q[2 * st], v3 = q[3 * st];
+      s += (v0 + v1) + (v2 + v3);
+    }
+    for (; p < n_part; p += 64) s += part[(long long)p * cols + col];
+  }
+  sums[p0][cl] = s;
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    const int c2 = threadIdx.x >> 4, l = threadIdx.x & 15, oc = blockIdx.x * 16 + c2;     // 16 lanes per column
+    float t = (sums[l][c2] + sums[l + 16][c2]) + (sums[l + 32][c2] + sums[l + 48][c2]);
+    t = lanes_sum<16>(t);
+    if (l == 0 && oc < cols) {
+      float* to = oc < split ? out0 : out1;      // null: not wanted
+      if (to) {
+        float* o = to + (oc < split ? oc : oc - split);
+        *o = accumulate ? *o + t : t;
+      }
+    }
+  }
+}

@@ -1,0 +1,515 @@
+// Operators around the block: layer norm, relative position embedding, activation checkpoints in 8 bits (see include/pe.h).
+// Host side: argument checks, the choice of kernel variants, launches.
+#include <stdio.h>
+#include <string.h>
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "pe_ckpt.h"
+#include "pe_handle.h"
+#include "pe_ln.h"
+#include "pe_ops.h"
+#include "pe_relpos.h"
+
+namespace {
+
+// One call of an operator: refusals with a text, launches with the handle's timing and checking options.
+struct OpCall {
+  pe_handle* h;
+  hipStream_t st;
+  int err = PE_OK;
+  int refuse(int code, const char* text) {
+    h->last_error = text;
+    return code;
+  }
+  // the current device is the handle's: the kernels are launched there, on a stream of it
+  bool device_ok() {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) { (void)hipGetLastError(); return false; }
+    return dev == h->device;
+  }
+  hipEvent_t event() {
+    hipEvent_t e;
+    if (!h->ev_pool.empty()) { e = h->ev_pool.back(); h->ev_pool.pop_back(); return e; }
+    if (hipEventCreate(&e) != hipSuccess) return nullptr;
+    return e;
+  }
+  template <typename F> void launch(const char* label, const char* kern, double flops, double bytes, F&& f) {
+    if (err) return;
+    hipEvent_t e0 = nullptr, e1 = nullptr;
+    if (h->timing && (e0 = event())) (void)hipEventRecord(e0, st);
+    f();
+    if (e0 && (e1 = event())) {
+      (void)hipEventRecord(e1, st);
+      h->recs.push_back(ProfRec{label, kern, flops, bytes, e0, e1});
+    }
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && h->sync_debug) e = hipStreamSynchronize(st);
+    if (e != hipSuccess) {
+      err = PE_ERR_HIP;
+      h->last_error = std::string(label) + ": " + hipGetErrorString(e);
+    }
+  }
+};
+
+// An entry point's body: nothing thrown (the host has run out of memory) passes the C boundary
+template <typename F> int guarded(F&& f) {
+  try { return f(); } catch (...) { return PE_ERR_HIP; }
+}
+
+size_t elem(int dtype) { return dtype == PE_BF16 ? 2 : 4; }
+bool type_ok(int dtype) { return dtype == PE_F32 || dtype == PE_BF16; }
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p) % a == 0; }
+// bytes from the first to the last element of [rows][c] with row stride ld
+size_t span(long long rows, long long c, long long ld, size_t e) { return rows > 0 && c > 0 ? ((size_t)(rows - 1) * ld + c) * e : 0; }
+
+// Elements per access: 8 (16-byte accesses), 2 or 1, whichever the channel count, the row strides and the addresses allow.
+struct Width {
+  int v;
+  size_t e;
+  Width(int c, size_t elem_bytes) : v(c % 8 == 0 ? 8 : c % 2 == 0 ? 2 : 1), e(elem_bytes) {}
+  Width& take(const void* p, long long ld, long long rows) {
+    if (!p) return *this;
+    if (rows <= 1) ld = 0;
+    if (v == 8 && (!aligned(p, 16) || (ld * (long long)e) % 16)) v = 2;
+    if (v == 2 && (!aligned(p, 2 * e) || ld % 2)) v = 1;
+    return *this;
+  }
+};
+
+constexpr int LN_MAX_C = 16384;
+constexpr long long MAX_ROWS = 1LL << 40;
+constexpr int CK_MAX_C = 1 << 20;
+
+// ---------------------------------------------------------------------------------------------------------------------
+// 8-bit checkpoints
+// ---------------------------------------------------------------------------------------------------------------------
+long long ck_groups(int c) { return (c + CK_GROUP - 1) / CK_GROUP; }
+size_t ck_bytes(long long rows, int c) { return up256((size_t)rows * c) + (size_t)rows * ck_groups(c); }
+
+template <typename T, int V, bool PACK>
+void ck_launch(hipStream_t st, const void* x, long long ld, void* ckpt, void* y, long long rows, int c) {
+  constexpr int U = V == 8 ? 4 : 8;
+  const int per_row = (int)ck_groups(c) * (CK_GROUP / V);
+  const long long items = rows * per_row, blocks = (items + 256 * U - 1) / (256 * U);
+  hipLaunchKernelGGL((ckpt_kernel<T, V, U, PACK>), dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
+                     (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row);
+}
+template <bool PACK> void ck_run(hipStream_t st, int dtype, int v, const void* x, long long ld, void* ckpt, void* y, long long rows, int c) {
+  if (dtype == PE_BF16) {
+    if (v == 8) ck_launch<bf16, 8, PACK>(st, x, ld, ckpt, y, rows, c);
+    else if (v == 2) ck_launch<bf16, 2, PACK>(st, x, ld, ckpt, y, rows, c);
+    else ck_launch<bf16, 1, PACK>(st, x, ld, ckpt, y, rows, c);
+  } else {
+    if (v == 8) ck_launch<float, 8, PACK>(st, x, ld, ckpt, y, rows, c);
+    else if (v == 2) ck_launch<float, 2, PACK>(st, x, ld, ckpt, y, rows, c);
+    else ck_launch<float, 1, PACK>(st, x, ld, ckpt, y, rows, c);
+  }
+}
+
+int ck_call(pe_handle* h, long long rows, int c, int dtype, const void* t, long long ld, const void* ckpt, bool pack, void* stream) {
+  if (!h) return PE_ERR_NULL;
+  OpCall op{h, (hipStream_t)stream};
+  if (rows < 0 || rows > MAX_ROWS || c < 1 || c > CK_MAX_C || !type_ok(dtype) || (double)rows * c > 1e12)
+    return op.refuse(PE_ERR_DIMS, "checkpoint: rows in [0, 2^40], c in [1, 2^20], rows * c up to 10^12, dtype PE_F32 or PE_BF16");
+  if (ld < c) return op.refuse(PE_ERR_ARG, "checkpoint: a row stride is less than c");
+  if (rows == 0) return PE_OK;
+  if (!t || !ckpt) return op.refuse(PE_ERR_NULL, "checkpoint: null tensor");
+  const size_t e = elem(dtype);
+  if (!aligned(t, e) || !aligned(ckpt, 256)) return op.refuse(PE_ERR_ARG, "checkpoint: a tensor is not aligned to its elements, or the checkpoint not to 256 bytes");
+  const Region rg[] = {{t, span(rows, c, ld, e), !pack}, {ckpt, ck_bytes(rows, c), pack}};
+  if (any_alias(rg, 2)) return op.refuse(PE_ERR_ALIAS, "checkpoint: tensor and checkpoint overlap");
+  if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "checkpoint: the handle belongs to another device than the current one");
+  const int v = Width(c, e).take(t, ld, rows).v;
+  const double n = (double)rows * c, bytes = n * e + ck_bytes(rows, c);
+  op.launch(pack ? "ckpt pack" : "ckpt unpack", "ckpt_kernel", 2 * n, bytes, [&] {
+    if (pack) ck_run<true>(op.st, dtype, v, t, ld, const_cast<void*>(ckpt), nullptr, rows, c);
+    else ck_run<false>(op.st, dtype, v, nullptr, ld, const_cast<void*>(ckpt), const_cast<void*>(t), rows, c);
+  });
+  return op.err;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Layer norm
+// ---------------------------------------------------------------------------------------------------------------------
+// Lanes and vectors per lane of a row of c channels in accesses of v elements
+struct LnPlan { int l, nv; int rows() const { return l > 256 ? 1 : 256 / l; } };
+LnPlan ln_plan(int c, int v) {
+  const int n = c / v;
+  if (v == 8) {
+    if (n <= 4) return {4, 1};
+    if (n <= 8) return {8, 1};
+    if (n <= 16) return {16, 1};
+    if (n <= 32) return {32, 1};
+    if (n <= 64) return {64, 1};
+    if (n <= 128) return {64, 2};
+    if (n <= 512) return {256, 2};
+    if (n <= 1024) return {512, 2};
+    return {1024, 2};
+  }
+  if (n <= 64) return {64, 1};
+  if (n <= 256) return {64, 4};
+  if (n <= 1024) return {256, 4};
+  if (n <= 4096) return {1024, 4};
+  return v == 2 ? LnPlan{1024, 8} : LnPlan{1024, 16};
+}
+constexpr int LN_FWD_WG = 2048, LN_BWD_WG = 1024;
+long long ln_bwd_groups(long long rows, int c, int v) {
+  const LnPlan p = ln_plan(c, v);
+  return std::min<long long>((rows + p.rows() - 1) / p.rows(), p.l <= 64 ? LN_BWD_WG : 512);
+}
+
+template <typename T, int V, int L, int NV> void ln_fwd_launch(hipStream_t st, const LnArgs& a) {
+  const long long wg = (a.rows + LnShape<L>::ROWS - 1) / LnShape<L>::ROWS;
+  hipLaunchKernelGGL((ln_op_fwd_kernel<T, V, L, NV>), dim3((unsigned)std::min<long long>(wg, LN_FWD_WG)), dim3(LnShape<L>::THREADS), 0, st, a);
+}
+template <typename T, int V, int L, int NV> void ln_bwd_launch(hipStream_t st, const LnArgs& a, unsigned wg) {
+  if (a.codes) hipLaunchKernelGGL((ln_op_bwd_kernel<T, V, L, NV, true>), dim3(wg), dim3(LnShape<L>::THREADS), 0, st, a);
+  else hipLaunchKernelGGL((ln_op_bwd_kernel<T, V, L, NV, false>), dim3(wg), dim3(LnShape<L>::THREADS), 0, st, a);
+}
+// calls `f` with the plan's template arguments
+template <int V, typename F> void ln_dispatch(const LnPlan& p, F&& f) {
+#define PE_LN_CASE(L, NV) if (p.l == L && p.nv == NV) return f(std::integral_constant<int, L>{}, std::integral_constant<int, NV>{})
+  if constexpr (V == 8) {
+    PE_LN_CASE(4, 1); PE_LN_CASE(8, 1); PE_LN_CASE(16, 1); PE_LN_CASE(32, 1); PE_LN_CASE(64, 1);
+    PE_LN_CASE(64, 2); PE_LN_CASE(256, 2); PE_LN_CASE(512, 2); PE_LN_CASE(1024, 2);
+  } else {
+    PE_LN_CASE(64, 1); PE_LN_CASE(64, 4); PE_LN_CASE(256, 4); PE_LN_CASE(1024, 4);
+    if constexpr (V == 2) { PE_LN_CASE(1024, 8); } else { PE_LN_CASE(1024, 16); }
+  }
+#undef PE_LN_CASE
+}
+template <typename T, int V> void ln_fwd_run(hipStream_t st, const LnArgs& a) {
+  ln_dispatch<V>(ln_plan(a.c, V), [&](auto l, auto nv) { ln_fwd_launch<T, V, l.value, nv.value>(st, a); });
+}
+template <typename T, int V> void ln_bwd_run(hipStream_t st, const LnArgs& a, unsigned wg) {
+  ln_dispatch<V>(ln_plan(a.c, V), [&](auto l, auto nv) { ln_bwd_launch<T, V, l.value, nv.value>(st, a, wg); });
+}
+void columns_sum(OpCall& op, const char* label, const float* part, long long n_part, int cols, float* o0, float* o1, int split, bool acc) {
+  op.launch(label, "columns_sum_kernel", (double)n_part * cols, 4.0 * ((double)n_part * cols + cols), [&] {
+    hipLaunchKernelGGL(columns_sum_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(1024), 0, op.st, part, (int)n_part, cols, o0, o1, split, (int)acc);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Relative positions
+// ---------------------------------------------------------------------------------------------------------------------
+int rp_buckets(const pe_relpos& p) { return p.n_edges + 1 + (p.segments ? 1 : 0); }
+const char* rp_why(const pe_relpos& p) {
+  if (p.n_q < 0 || p.n_k < 0 || p.n_q > (1 << 27) || p.n_k > (1 << 27)) return "relative positions: n_q and n_k in [0, 2^27]";
+  if (p.c < 1 || p.c > 1024) return "relative positions: c in [1, 1024]";
+  if ((double)p.n_q * p.n_k * p.c > 1e12) return "relative positions: n_q * n_k * c up to 10^12";
+  if (p.n_edges < 0 || p.n_edges > RP_MAX_EDGES) return "relative positions: n_edges in [0, 254]";
+  if (p.layout != PE_RELPOS_PAIR && p.layout != PE_RELPOS_HEADS) return "relative positions: layout PE_RELPOS_PAIR or PE_RELPOS_HEADS";
+  if (p.segments != 0 && p.segments != 1) return "relative positions: segments 0 or 1";
+  if (!type_ok(p.dtype)) return "relative positions: dtype PE_F32 or PE_BF16";
+  if (p.ld < 0) return "relative positions: ld at least 0";
+  return nullptr;
+}
+long long rp_row(const pe_relpos& p) { return p.layout == PE_RELPOS_PAIR ? (long long)p.n_k * p.c : p.n_k; }
+long long rp_ld(const pe_relpos& p) { return p.ld ? p.ld : rp_row(p); }
+
+// waves per workgroup of the backward kernels: each has accumulators of its own, [buckets][64] in LDS (160 KB, of which the edges
+// take one)
+int rp_waves(int nb) { return std::max(1, std::min(8, (int)(150 * 1024 / (nb * 256)))); }
+size_t rp_lds(int nb, int waves) { return (size_t)waves * nb * 256 + 4 * (RP_MAX_EDGES + 2); }
+// PAIR: position groups.  Partial sums cost 8 bytes per group, bucket and channel: a group has at least 512 positions
+long long rp_pair_groups(const pe_relpos& p) {
+  const long long n = (long long)p.n_q * p.n_k;
+  return std::max<long long>(1, std::min<long long>(128, (n + 511) / 512));
+}
+// HEADS: rows q per workgroup, so that about 512 workgroups share the work
+int rp_heads_rows(const pe_relpos& p, int v) {
+  const long long tiles = (p.n_k + 64LL * v - 1) / (64LL * v) * p.c;
+  const long long split = std::max<long long>(1, (512 + tiles - 1) / tiles);
+  const long long least = 8;      // a row for each wave
+  return (int)std::max<long long>(least, (p.n_q + split - 1) / split);
+}
+long long rp_heads_groups(const pe_relpos& p, int v) {
+  const int rows = rp_heads_rows(p, v);
+  return (long long)((p.n_k + 64 * v - 1) / (64 * v)) * ((p.n_q + rows - 1) / rows);
+}
+size_t rp_workspace(const pe_relpos& p) {
+  if (p.n_q == 0 || p.n_k == 0) return 256;
+  const long long g = p.layout == PE_RELPOS_PAIR ? rp_pair_groups(p)
+                                                 : std::max(rp_heads_groups(p, 8), std::max(rp_heads_groups(p, 2), rp_heads_groups(p, 1)));
+  return up256((size_t)g * rp_buckets(p) * p.c * 4);
+}
+
+// The checks that forward and backward share; on PE_OK `a` is filled but for the tensors of the direction
+int rp_check(OpCall& op, const pe_relpos* p, const int* edges, const int* pos_q, const int* pos_k, const int* seg_q, const int* seg_k, RpArgs& a) {
+  if (!p) return op.refuse(PE_ERR_NULL, "relative positions: null description");
+  if (const char* why = rp_why(*p)) return op.refuse(PE_ERR_DIMS, why);
+  if (p->ld && p->ld < rp_row(*p)) return op.refuse(PE_ERR_ARG, "relative positions: ld is less than a row");
+  if (p->n_edges && !edges) return op.refuse(PE_ERR_NULL, "relative positions: null edges");
+  a.dense = p->n_edges > 0;
+  for (int i = 0; i < p->n_edges; i++) {
+    if (edges[i] == -2147483647 - 1 || (i && edges[i] <= edges[i - 1])) return op.refuse(PE_ERR_ARG, "relative positions: edges have to ascend, the first above -2^31");
+    if (i && edges[i] != edges[i - 1] + 1) a.dense = 0;
+    a.edges[i] = edges[i];
+  }
+  const bool some = p->n_q > 0 && p->n_k > 0;
+  if (some && (!pos_q || !pos_k || (p->segments && (!seg_q || !seg_k)))) return op.refuse(PE_ERR_NULL, "relative positions: null positions or segments");
+  if (!aligned(pos_q, 4) || !aligned(pos_k, 4) || !aligned(seg_q, 4) || !aligned(seg_k, 4)) return op.refuse(PE_ERR_ARG, "relative positions: a tensor is not aligned to its elements");
+  a.pos_q = pos_q; a.pos_k = pos_k;
+  a.seg_q = p->segments ? seg_q : nullptr; a.seg_k = p->segments ? seg_k : nullptr;
+  a.table = nullptr; a.add = nullptr; a.out = nullptr; a.d_out = nullptr; a.part = nullptr;
+  a.ld = rp_ld(*p);
+  a.n_q = p->n_q; a.n_k = p->n_k; a.c = p->c; a.nb = rp_buckets(*p); a.n_edges = p->n_edges;
+  return PE_OK;
+}
+size_t rp_span(const pe_relpos& p) {
+  return p.layout == PE_RELPOS_PAIR ? span(p.n_q, rp_row(p), rp_ld(p), elem(p.dtype))
+                                    : span((long long)p.n_q * p.c, rp_row(p), rp_ld(p), elem(p.dtype));
+}
+
+template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
+  constexpr int U = V == 8 ? 4 : 8;
+  const int vecs = a.c / V;
+  const int tile = std::max(1, std::min(1024, 256 * U / vecs));          // vecs <= 1024 (c <= 1024): at least one position
+  const unsigned gx = (unsigned)((a.n_k + tile - 1) / tile), gy = (unsigned)std::min(a.n_q, 65535), gz = (unsigned)((a.n_q + 65534) / 65535);
+  hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile);
+}
+template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) {
+  // heads per workgroup: what 32 KB of LDS hold, and few enough that the chip is filled
+  const long long tiles = (a.n_k + 256LL * V - 1) / (256LL * V);
+  int heads = std::max(1, std::min(a.c, 32 * 1024 / (a.nb * 4)));
+  while (heads > 1 && tiles * a.n_q * ((a.c + heads - 1) / heads) < 512) heads = (heads + 1) / 2;
+  const unsigned gz = (unsigned)((a.c + heads - 1) / heads);
+  // rows per workgroup: the table's copy in LDS is shared by as many rows as leave 2048 workgroups
+  const long long all = tiles * gz;
+  const int rows = (int)std::max<long long>((a.n_q + 65534) / 65535, std::min<long long>(16, a.n_q * all / 2048));
+  hipLaunchKernelGGL((relpos_heads_fwd_kernel<T, V>), dim3((unsigned)tiles, (unsigned)((a.n_q + rows - 1) / rows), gz), dim3(256),
+                     (size_t)heads * a.nb * 4, st, a, heads, rows);
+}
+template <typename T> void rp_fwd_run(hipStream_t st, const RpArgs& a, int layout, int v) {
+  if (layout == PE_RELPOS_PAIR) {
+    if (v == 8) rp_pair_fwd<T, 8>(st, a); else if (v == 2) rp_pair_fwd<T, 2>(st, a); else rp_pair_fwd<T, 1>(st, a);
+  } else {
+    if (v == 8) rp_heads_fwd<T, 8>(st, a); else if (v == 2) rp_heads_fwd<T, 2>(st, a); else rp_heads_fwd<T, 1>(st, a);
+  }
+}
+// Dynamic LDS above 64 KB has to be allowed once per kernel and device
+template <typename K> void allow_lds(K kern) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return;      // the launch reports it
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (done.load() & bit) return;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024) == hipSuccess) done |= bit;
+}
+template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, const RpArgs& a, long long groups) {
+  const int waves = rp_waves(a.nb);
+  const long long n = (long long)a.n_q * a.n_k;
+  allow_lds(&relpos_pair_bwd_kernel<T, S, U>);
+  hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, U>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(64 * waves), rp_lds(a.nb, waves), st,
+                     a, (n + groups - 1) / groups);
+}
+template <typename T, int V> void rp_heads_bwd(hipStream_t st, const RpArgs& a, int rows) {
+  const int waves = rp_waves(a.nb);
+  allow_lds(&relpos_heads_bwd_kernel<T, V>);
+  hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V>), dim3((unsigned)((a.n_k + 64 * V - 1) / (64 * V)), (unsigned)((a.n_q + rows - 1) / rows), (unsigned)a.c),
+                     dim3(64 * waves), rp_lds(a.nb, waves), st, a, rows);
+}
+template <typename T> void rp_bwd_run(hipStream_t st, const RpArgs& a, int layout, int v, long long groups, int rows) {
+  if (layout == PE_RELPOS_PAIR) {
+    if (a.c > 32) rp_pair_bwd<T, 1, 16>(st, a, groups);
+    else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, a, groups);
+    else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, a, groups);
+    else rp_pair_bwd<T, 8, 8>(st, a, groups);
+  } else {
+    if (v == 8) rp_heads_bwd<T, 8>(st, a, rows); else if (v == 2) rp_heads_bwd<T, 2>(st, a, rows); else rp_heads_bwd<T, 1>(st, a, rows);
+  }
+}
+
+}  // namespace
+
+hipError_t ckpt_pack_launch(hipStream_t st, int dtype, const void* x, void* ckpt, long long rows, int c) {
+  ck_run<true>(st, dtype, 8, x, c, ckpt, nullptr, rows, c);
+  return hipGetLastError();
+}
+hipError_t ckpt_unpack_launch(hipStream_t st, int dtype, const void* ckpt, void* y, long long rows, int c) {
+  ck_run<false>(st, dtype, 8, nullptr, c, const_cast<void*>(ckpt), y, rows, c);
+  return hipGetLastError();
+}
+
+extern "C" {
+
+int pe_handle_device(const pe_handle* h) { return h ? h->device : PE_ERR_NULL; }
+
+size_t pe_ckpt_bytes(long long rows, int c) {
+  if (rows < 0 || rows > MAX_ROWS || c < 1 || c > CK_MAX_C || (double)rows * c > 1e12) return 0;
+  return ck_bytes(rows, c);
+}
+int pe_ckpt_pack(pe_handle* h, long long rows, int c, int dtype, const void* x, long long ld_x, void* ckpt, void* stream) {
+  return guarded([&] { return ck_call(h, rows, c, dtype, x, ld_x, ckpt, true, stream); });
+}
+int pe_ckpt_unpack(pe_handle* h, long long rows, int c, int dtype, const void* ckpt, void* y, long long ld_y, void* stream) {
+  return guarded([&] { return ck_call(h, rows, c, dtype, y, ld_y, ckpt, false, stream); });
+}
+
+size_t pe_layernorm_workspace_bytes(long long rows, int c) {
+  if (rows < 0 || rows > MAX_ROWS || c < 1 || c > LN_MAX_C) return 0;
+  long long g = 1;
+  for (int v : {8, 2, 1})
+    if (c % v == 0) g = std::max(g, ln_bwd_groups(rows, c, v));
+  return up256((size_t)g * 2 * c * 4);
+}
+
+int pe_layernorm_fwd(pe_handle* h, long long rows, int c, int dtype, const void* x, long long ld_x, const void* add, long long ld_add,
+                     const float* gain, const float* offset, float eps, void* y, long long ld_y, float* stats, void* ckpt, void* stream) {
+  return guarded([&]() -> int {
+    if (!h) return PE_ERR_NULL;
+    OpCall op{h, (hipStream_t)stream};
+    if (rows < 0 || rows > MAX_ROWS || c < 1 || c > LN_MAX_C || !type_ok(dtype))
+      return op.refuse(PE_ERR_DIMS, "layer norm: rows in [0, 2^40], c in [1, 16384], dtype PE_F32 or PE_BF16");
+    if (!(eps > 0.0f)) return op.refuse(PE_ERR_DIMS, "layer norm: eps has to be positive");
+    if (ld_x < c || ld_y < c || (add && ld_add < c)) return op.refuse(PE_ERR_ARG, "layer norm: a row stride is less than c");
+    if (rows == 0) return PE_OK;
+    if (!x || !y) return op.refuse(PE_ERR_NULL, "layer norm: null tensor");
+    const size_t e = elem(dtype);
+    if (!aligned(x, e) || !aligned(y, e) || !aligned(add, e) || !aligned(gain, 4) || !aligned(offset, 4) || !aligned(stats, 8) || !aligned(ckpt, 256))
+      return op.refuse(PE_ERR_ARG, "layer norm: a tensor is not aligned to its elements, stats not to 8 bytes, or the checkpoint not to 256");
+    const bool in_place = add == y && ld_add == ld_y;      // y = y + LN(x): every element is read by the lane that writes it
+    const Region rg[] = {{x, span(rows, c, ld_x, e), false}, {in_place ? nullptr : add, span(rows, c, ld_add, e), false},
+                         {gain, (size_t)c * 4, false}, {offset, (size_t)c * 4, false}, {y, span(rows, c, ld_y, e), true},
+                         {stats, (size_t)rows * 8, true}, {ckpt, ck_bytes(rows, c), true}};
+    if (any_alias(rg, 7)) return op.refuse(PE_ERR_ALIAS, "layer norm: a buffer that is written overlaps another one");
+    if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "layer norm: the handle belongs to another device than the current one");
+    LnArgs a{};
+    a.x = x; a.ld_x = ld_x; a.add = add; a.ld_add = ld_add; a.out = y; a.ld_out = ld_y; a.gain = gain; a.offset = offset; a.stats = stats;
+    a.rows = rows; a.c = c; a.eps = eps;
+    if (ckpt) { a.k_codes = (int8_t*)ckpt; a.k_scales = (uint8_t*)ckpt + up256((size_t)rows * c); }
+    const int v = Width(c, e).take(x, ld_x, rows).take(add, ld_add, rows).take(y, ld_y, rows).v;
+    const double n = (double)rows * c;
+    op.launch("layernorm fwd", "ln_op_fwd_kernel", 9 * n, n * e * (add ? 3 : 2) + (ckpt ? (double)ck_bytes(rows, c) : 0.0), [&] {
+      if (dtype == PE_BF16) { if (v == 8) ln_fwd_run<bf16, 8>(op.st, a); else if (v == 2) ln_fwd_run<bf16, 2>(op.st, a); else ln_fwd_run<bf16, 1>(op.st, a); }
+      else { if (v == 8) ln_fwd_run<float, 8>(op.st, a); else if (v == 2) ln_fwd_run<float, 2>(op.st, a); else ln_fwd_run<float, 1>(op.st, a); }
+    });
+    return op.err;
+  });
+}
+
+int pe_layernorm_bwd(pe_handle* h, long long rows, int c, int dtype, int x_type, const void* x, long long ld_x, const float* stats,
+                     const float* gain, const void* dy, long long ld_dy, const void* add, long long ld_add, void* dx, long long ld_dx,
+                     float* d_gain, float* d_offset, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> int {
+    if (!h) return PE_ERR_NULL;
+    OpCall op{h, (hipStream_t)stream};
+    if (rows < 0 || rows > MAX_ROWS || c < 1 || c > LN_MAX_C || !type_ok(dtype))
+      return op.refuse(PE_ERR_DIMS, "layer norm: rows in [0, 2^40], c in [1, 16384], dtype PE_F32 or PE_BF16");
+    const bool kept = x_type == PE_CKPT;
+    if (!kept && x_type != dtype) return op.refuse(PE_ERR_ARG, "layer norm: x is of the type dtype or a checkpoint (PE_CKPT)");
+    if ((!kept && ld_x < c) || ld_dy < c || (add && dx && ld_add < c) || (dx && ld_dx < c)) return op.refuse(PE_ERR_ARG, "layer norm: a row stride is less than c");
+    const bool params = d_gain || d_offset;
+    if (rows && (!x || !stats || !dy)) return op.refuse(PE_ERR_NULL, "layer norm: null tensor");
+    if (params && !workspace) return op.refuse(PE_ERR_NULL, "layer norm: the gradients of gain and offset need a workspace");
+    if (!dx) add = nullptr;
+    const size_t e = elem(dtype);
+    if (!aligned(x, kept ? 256 : e) || !aligned(dy, e) || !aligned(add, e) || !aligned(dx, e) || !aligned(gain, 4) || !aligned(stats, 8) ||
+        !aligned(d_gain, 4) || !aligned(d_offset, 4) || !aligned(workspace, 256))
+      return op.refuse(PE_ERR_ARG, "layer norm: a tensor is not aligned to its elements, stats not to 8 bytes, or the checkpoint or workspace not to 256");
+    const size_t need = params ? pe_layernorm_workspace_bytes(rows, c) : 0;
+    if (params && workspace_bytes < need) return op.refuse(PE_ERR_WORKSPACE, "layer norm: the workspace is smaller than pe_layernorm_workspace_bytes");
+    const bool in_place = add == dx && ld_add == ld_dx;    // dx = dx + ...
+    const Region rg[] = {{x, kept ? ck_bytes(rows, c) : span(rows, c, ld_x, e), false}, {stats, (size_t)rows * 8, false}, {gain, (size_t)c * 4, false},
+                         {dy, span(rows, c, ld_dy, e), false}, {in_place ? nullptr : add, span(rows, c, ld_add, e), false},
+                         {dx, span(rows, c, ld_dx, e), true}, {d_gain, (size_t)c * 4, true}, {d_offset, (size_t)c * 4, true},
+                         {params ? workspace : nullptr, need, true}};
+    if (any_alias(rg, 9)) return op.refuse(PE_ERR_ALIAS, "layer norm: a buffer that is written overlaps another one");
+    if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "layer norm: the handle belongs to another device than the current one");
+    long long groups = 0;
+    if (rows && (dx || params)) {
+      LnArgs a{};
+      if (kept) { a.codes = (const int8_t*)x; a.scales = (const uint8_t*)x + up256((size_t)rows * c); }
+      else { a.x = x; a.ld_x = ld_x; }
+      a.add = add; a.ld_add = ld_add; a.dy = dy; a.ld_dy = ld_dy; a.out = dx; a.ld_out = ld_dx; a.gain = gain; a.stats_in = stats;
+      a.part = params ? (float*)workspace : nullptr;
+      a.rows = rows; a.c = c;
+      const int v = Width(c, e).take(a.x, ld_x, rows).take(dy, ld_dy, rows).take(add, ld_add, rows).take(dx, ld_dx, rows).v;
+      groups = ln_bwd_groups(rows, c, v);
+      const unsigned wg = (unsigned)groups;
+      const double n = (double)rows * c;
+      op.launch("layernorm bwd", "ln_op_bwd_kernel", 15 * n, n * e * (1 + (dx ? 1 : 0) + (add ? 1 : 0)) + (kept ? (double)ck_bytes(rows, c) : n * e), [&] {
+        if (dtype == PE_BF16) { if (v == 8) ln_bwd_run<bf16, 8>(op.st, a, wg); else if (v == 2) ln_bwd_run<bf16, 2>(op.st, a, wg); else ln_bwd_run<bf16, 1>(op.st, a, wg); }
+        else { if (v == 8) ln_bwd_run<float, 8>(op.st, a, wg); else if (v == 2) ln_bwd_run<float, 2>(op.st, a, wg); else ln_bwd_run<float, 1>(op.st, a, wg); }
+      });
+    }
+    if (params && (groups || !accumulate)) columns_sum(op, "layernorm sums", (const float*)workspace, groups, 2 * c, d_gain, d_offset, c, accumulate != 0);
+    return op.err;
+  });
+}
+
+size_t pe_relpos_workspace_bytes(const pe_relpos* p) {
+  if (!p || rp_why(*p)) return 0;
+  return rp_workspace(*p);
+}
+
+int pe_relpos_fwd(pe_handle* h, const pe_relpos* p, const int* edges, const int* pos_q, const int* pos_k, const int* seg_q, const int* seg_k,
+                  const float* table, const void* add, void* out, void* stream) {
+  return guarded([&]() -> int {
+    if (!h) return PE_ERR_NULL;
+    OpCall op{h, (hipStream_t)stream};
+    RpArgs a;
+    int rc = rp_check(op, p, edges, pos_q, pos_k, seg_q, seg_k, a);
+    if (rc) return rc;
+    if (p->n_q == 0 || p->n_k == 0) return PE_OK;
+    if (!table || !out) return op.refuse(PE_ERR_NULL, "relative positions: null tensor");
+    const size_t e = elem(p->dtype);
+    if (!aligned(table, 4) || !aligned(add, e) || !aligned(out, e)) return op.refuse(PE_ERR_ARG, "relative positions: a tensor is not aligned to its elements");
+    const Region rg[] = {{pos_q, (size_t)p->n_q * 4, false}, {pos_k, (size_t)p->n_k * 4, false}, {a.seg_q, (size_t)p->n_q * 4, false},
+                         {a.seg_k, (size_t)p->n_k * 4, false}, {table, (size_t)a.nb * p->c * 4, false},
+                         {add == out ? nullptr : add, rp_span(*p), false}, {out, rp_span(*p), true}};
+    if (any_alias(rg, 7)) return op.refuse(PE_ERR_ALIAS, "relative positions: the output overlaps another buffer");
+    if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "relative positions: the handle belongs to another device than the current one");
+    a.table = table; a.add = add; a.out = out;
+    const bool pair = p->layout == PE_RELPOS_PAIR;
+    const int v = Width(pair ? p->c : p->n_k, e).take(add, a.ld, 2).take(out, a.ld, 2).v;
+    const double n = (double)p->n_q * p->n_k * p->c;
+    op.launch("relpos fwd", pair ? "relpos_pair_fwd_kernel" : "relpos_heads_fwd_kernel", n, n * e * (add ? 2 : 1), [&] {
+      if (p->dtype == PE_BF16) rp_fwd_run<bf16>(op.st, a, p->layout, v); else rp_fwd_run<float>(op.st, a, p->layout, v);
+    });
+    return op.err;
+  });
+}
+
+int pe_relpos_bwd(pe_handle* h, const pe_relpos* p, const int* edges, const int* pos_q, const int* pos_k, const int* seg_q, const int* seg_k,
+                  const void* d_out, float* d_table, int accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> int {
+    if (!h) return PE_ERR_NULL;
+    OpCall op{h, (hipStream_t)stream};
+    RpArgs a;
+    int rc = rp_check(op, p, edges, pos_q, pos_k, seg_q, seg_k, a);
+    if (rc) return rc;
+    const bool some = p->n_q > 0 && p->n_k > 0;
+    if (!d_table || !workspace || (some && !d_out)) return op.refuse(PE_ERR_NULL, "relative positions: null tensor or workspace");
+    const size_t e = elem(p->dtype), need = rp_workspace(*p);
+    if (!aligned(d_out, e) || !aligned(d_table, 4) || !aligned(workspace, 256))
+      return op.refuse(PE_ERR_ARG, "relative positions: a tensor is not aligned to its elements, or the workspace not to 256 bytes");
+    if (workspace_bytes < need) return op.refuse(PE_ERR_WORKSPACE, "relative positions: the workspace is smaller than pe_relpos_workspace_bytes");
+    const Region rg[] = {{pos_q, (size_t)p->n_q * 4, false}, {pos_k, (size_t)p->n_k * 4, false}, {a.seg_q, (size_t)p->n_q * 4, false},
+                         {a.seg_k, (size_t)p->n_k * 4, false}, {d_out, rp_span(*p), false}, {d_table, (size_t)a.nb * p->c * 4, true},
+                         {workspace, need, true}};
+    if (any_alias(rg, 7)) return op.refuse(PE_ERR_ALIAS, "relative positions: a buffer that is written overlaps another one");
+    if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "relative positions: the handle belongs to another device than the current one");
+    a.d_out = d_out; a.part = (float*)workspace;
+    const bool pair = p->layout == PE_RELPOS_PAIR;
+    long long groups = 0;
+    if (some) {
+      const int v = pair ? 1 : Width(p->n_k, e).take(d_out, a.ld, 2).v;
+      const int rows = pair ? 0 : rp_heads_rows(*p, v);
+      groups = pair ? rp_pair_groups(*p) : rp_heads_groups(*p, v);
+      const double n = (double)p->n_q * p->n_k * p->c;
+      op.launch("relpos bwd", pair ? "relpos_pair_bwd_kernel" : "relpos_heads_bwd_kernel", n, n * e, [&] {
+        if (p->dtype == PE_BF16) rp_bwd_run<bf16>(op.st, a, p->layout, v, groups, rows); else rp_bwd_run<float>(op.st, a, p->layout, v, groups, rows);
+      });
+    }
+    const int cols = a.nb * p->c;
+    if (groups || !accumulate) columns_sum(op, "relpos sums", (const float*)workspace, groups, cols, d_table, nullptr, cols, accumulate != 0);
+    return op.err;
+  });
+}
+
+}  // extern "C"
