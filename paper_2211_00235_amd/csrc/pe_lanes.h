@@ -72,3 +72,19 @@ template <typename T, int V> PE_DEV Raw<T, V> raw_zero() {
   for (int i = 0; i < V; i++) r.set(i, 0.0f);
   return r;
 }
+
+// V consecutive fp32 numbers at an address of which only 4-byte alignment is known, in as few accesses as there are 16-byte pieces
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2_u __attribute__((ext_vector_type(2), aligned(4)));
+template <int V> PE_DEV void load_f32(const float* p, float (&v)[V]) {
+  if constexpr (V == 8) {
+    const f32x4_u a = *reinterpret_cast<const f32x4_u*>(p), b = *reinterpret_cast<const f32x4_u*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; i++) { v[i] = a[i]; v[4 + i] = b[i]; }
+  } else if constexpr (V == 2) {
+    const f32x2_u a = *reinterpret_cast<const f32x2_u*>(p);
+    v[0] = a[0]; v[1] = a[1];
+  } else {
+    v[0] = *p;
+  }
+}

@@ -59,15 +59,13 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
   bool in[NV];
 #pragma unroll
   for (int n = 0; n < NV; n++) in[n] = n * L + li < n_vec;
-  constexpr bool HELD = NV * V <= 8;      // gain and offset stay in registers, and the next row is requested ahead
-  auto gain_of = [&](int n, int i) { return in[n] && a.gain ? a.gain[(n * L + li) * V + i] : 1.0f; };
-  auto offs_of = [&](int n, int i) { return in[n] && a.offset ? a.offset[(n * L + li) * V + i] : 0.0f; };
-  float gain[HELD ? NV : 1][V], offs[HELD ? NV : 1][V];
-  if constexpr (HELD) {
+  float gain[NV][V], offs[NV][V];
 #pragma unroll
-    for (int n = 0; n < NV; n++)
+  for (int n = 0; n < NV; n++) {
 #pragma unroll
-      for (int i = 0; i < V; i++) { gain[n][i] = gain_of(n, i); offs[n][i] = offs_of(n, i); }
+    for (int i = 0; i < V; i++) { gain[n][i] = 1.0f; offs[n][i] = 0.0f; }
+    if (in[n] && a.gain) load_f32<V>(a.gain + (n * L + li) * V, gain[n]);
+    if (in[n] && a.offset) load_f32<V>(a.offset + (n * L + li) * V, offs[n]);
   }
   const T* x = (const T*)a.x;
   const T* add = (const T*)a.add;
@@ -80,11 +78,10 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
     for (int n = 0; n < NV; n++)
       next[n] = in[n] && r < a.rows ? raw_load<T, V>(x + r * a.ld_x + (n * L + li) * V) : raw_zero<T, V>();
   };
-  if constexpr (HELD) fetch(row);
+  fetch(row);
   int slot = 0;
   for (; row < a.rows; row += step, slot ^= 2) {
     Raw<T, V> v[NV], ad[NV];
-    if constexpr (!HELD) fetch(row);
 #pragma unroll
     for (int n = 0; n < NV; n++) v[n] = next[n];
     if (add) {
@@ -92,7 +89,7 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
       for (int n = 0; n < NV; n++)
         if (in[n]) ad[n] = raw_load<T, V>(add + row * a.ld_add + (n * L + li) * V);
     }
-    if constexpr (HELD) fetch(row + step);
+    fetch(row + step);
     float s = 0.0f;
 #pragma unroll
     for (int n = 0; n < NV; n++)
@@ -114,9 +111,7 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
       Raw<T, V> o;
 #pragma unroll
       for (int i = 0; i < V; i++) {
-        float g, b;
-        if constexpr (HELD) { g = gain[n][i]; b = offs[n][i]; } else { g = gain_of(n, i); b = offs_of(n, i); }
-        float f = (v[n].get(i) - mean) * rstd * g + b;
+        float f = (v[n].get(i) - mean) * rstd * gain[n][i] + offs[n][i];
         if (add) f += ad[n].get(i);
         o.set(i, f);
       }
@@ -149,19 +144,13 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
   bool in[NV];
 #pragma unroll
   for (int n = 0; n < NV; n++) in[n] = n * L + li < n_vec;
-  constexpr bool HELD = NV * V <= 8;
-  auto gain_of = [&](int n, int i) { return in[n] && a.gain ? a.gain[(n * L + li) * V + i] : 1.0f; };
-  float gain[HELD ? NV : 1][V], dg[NV][V], db[NV][V];
+  float gain[NV][V], dg[NV][V], db[NV][V];
 #pragma unroll
-  for (int n = 0; n < NV; n++)
+  for (int n = 0; n < NV; n++) {
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-      if constexpr (HELD) gain[n][i] = gain_of(n, i);
-      dg[n][i] = db[n][i] = 0.0f;
-    }
-  auto u_of = [&](int n, int i, float d) {
-    if constexpr (HELD) return d * gain[n][i]; else return d * gain_of(n, i);
-  };
+    for (int i = 0; i < V; i++) { gain[n][i] = 1.0f; dg[n][i] = db[n][i] = 0.0f; }
+    if (in[n] && a.gain) load_f32<V>(a.gain + (n * L + li) * V, gain[n]);
+  }
   const T* x = (const T*)a.x;
   const T* dy = (const T*)a.dy;
   const T* add = (const T*)a.add;
@@ -192,13 +181,14 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
       }
     }
   };
-  if constexpr (HELD) fetch(row);
+  constexpr bool AHEAD = L <= 512;      // the next row is requested ahead; 1024 lanes have 128 registers each, too few for it
+  if constexpr (AHEAD) fetch(row);
   int slot = 0;
   for (; row < a.rows; row += step, slot ^= 2) {
     Raw<T, V> y[NV], ad[NV], xv[NV];
     Codes<V> cd[NV];
     float sc[NV];
-    if constexpr (!HELD) fetch(row);
+    if constexpr (!AHEAD) fetch(row);
     const float mean = nst[0], rstd = nst[1];
 #pragma unroll
     for (int n = 0; n < NV; n++) {
@@ -210,7 +200,7 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
       for (int n = 0; n < NV; n++)
         if (in[n]) ad[n] = raw_load<T, V>(add + row * a.ld_add + (n * L + li) * V);
     }
-    if constexpr (HELD) fetch(row + step);
+    if constexpr (AHEAD) fetch(row + step);
     auto z_of = [&](int n, int i) {
       float f;
       if constexpr (KEPT) f = (float)cd[n].get(i) * sc[n]; else f = xv[n].get(i);
@@ -221,7 +211,7 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
     for (int n = 0; n < NV; n++)
 #pragma unroll
       for (int i = 0; i < V; i++) {
-        const float d = y[n].get(i), z = in[n] ? z_of(n, i) : 0.0f, u = u_of(n, i, d);
+        const float d = y[n].get(i), z = in[n] ? z_of(n, i) : 0.0f, u = d * gain[n][i];
         dg[n][i] += d * z;
         db[n][i] += d;
         s1 += u;
@@ -234,7 +224,7 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
         Raw<T, V> o;
 #pragma unroll
         for (int i = 0; i < V; i++) {
-          float f = rstd * (u_of(n, i, y[n].get(i)) - m1 - z_of(n, i) * m2);
+          float f = rstd * (y[n].get(i) * gain[n][i] - m1 - z_of(n, i) * m2);
           if (add) f += ad[n].get(i);
           o.set(i, f);
         }

@@ -212,9 +212,9 @@ long long rp_row(const pe_relpos& p) { return p.layout == PE_RELPOS_PAIR ? (long
 long long rp_ld(const pe_relpos& p) { return p.ld ? p.ld : rp_row(p); }
 
 // waves per workgroup of the backward kernels: each has accumulators of its own, [buckets][64] in LDS (160 KB, of which the edges
-// take one)
+// take up to 4)
 int rp_waves(int nb) { return std::max(1, std::min(8, (int)(150 * 1024 / (nb * 256)))); }
-size_t rp_lds(int nb, int waves) { return (size_t)waves * nb * 256 + 4 * (RP_MAX_EDGES + 2); }
+size_t rp_lds(int nb, int waves, int mode) { return (size_t)waves * nb * 256 + 4 * rp_lds_words(mode); }
 // PAIR: position groups.  Partial sums cost 8 bytes per group, bucket and channel: a group has at least 512 positions
 long long rp_pair_groups(const pe_relpos& p) {
   const long long n = (long long)p.n_q * p.n_k;
@@ -244,12 +244,15 @@ int rp_check(OpCall& op, const pe_relpos* p, const int* edges, const int* pos_q,
   if (const char* why = rp_why(*p)) return op.refuse(PE_ERR_DIMS, why);
   if (p->ld && p->ld < rp_row(*p)) return op.refuse(PE_ERR_ARG, "relative positions: ld is less than a row");
   if (p->n_edges && !edges) return op.refuse(PE_ERR_NULL, "relative positions: null edges");
-  a.dense = p->n_edges > 0;
+  bool dense = true;
   for (int i = 0; i < p->n_edges; i++) {
     if (edges[i] == -2147483647 - 1 || (i && edges[i] <= edges[i - 1])) return op.refuse(PE_ERR_ARG, "relative positions: edges have to ascend, the first above -2^31");
-    if (i && edges[i] != edges[i - 1] + 1) a.dense = 0;
+    if (i && edges[i] != edges[i - 1] + 1) dense = false;
     a.edges[i] = edges[i];
   }
+  a.lo = p->n_edges ? edges[0] - 1 : 0;
+  a.hi = p->n_edges ? edges[p->n_edges - 1] : 0;
+  a.mode = dense ? RP_DENSE : (long long)a.hi - a.lo < RP_LUT ? RP_LUTS : RP_SEARCH;
   const bool some = p->n_q > 0 && p->n_k > 0;
   if (some && (!pos_q || !pos_k || (p->segments && (!seg_q || !seg_k)))) return op.refuse(PE_ERR_NULL, "relative positions: null positions or segments");
   if (!aligned(pos_q, 4) || !aligned(pos_k, 4) || !aligned(seg_q, 4) || !aligned(seg_k, 4)) return op.refuse(PE_ERR_ARG, "relative positions: a tensor is not aligned to its elements");
@@ -265,12 +268,19 @@ size_t rp_span(const pe_relpos& p) {
                                     : span((long long)p.n_q * p.c, rp_row(p), rp_ld(p), elem(p.dtype));
 }
 
+// calls `f` with the mode as a template argument
+template <typename F> void rp_dispatch(int mode, F&& f) {
+  if (mode == RP_DENSE) f(std::integral_constant<int, RP_DENSE>{});
+  else if (mode == RP_LUTS) f(std::integral_constant<int, RP_LUTS>{});
+  else f(std::integral_constant<int, RP_SEARCH>{});
+}
 template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
   constexpr int U = V == 8 ? 4 : 8;
   const int vecs = a.c / V;
-  const int tile = std::max(1, std::min(1024, 256 * U / vecs));          // vecs <= 1024 (c <= 1024): at least one position
+  const int tile = std::max(1, 256 * U / vecs);          // vecs <= 1024 <= 256 U (c <= 1024): at least one position
+  const unsigned magic = vecs == 1 ? 0u : (unsigned)(((1ull << 32) + vecs - 1) / vecs);     // exact for vectors up to 2^11
   const unsigned gx = (unsigned)((a.n_k + tile - 1) / tile), gy = (unsigned)std::min(a.n_q, 65535), gz = (unsigned)((a.n_q + 65534) / 65535);
-  hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile);
+  rp_dispatch(a.mode, [&](auto m) { hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U, m.value>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile, magic); });
 }
 template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) {
   // heads per workgroup: what 32 KB of LDS hold, and few enough that the chip is filled
@@ -281,8 +291,10 @@ template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) 
   // rows per workgroup: the table's copy in LDS is shared by as many rows as leave 2048 workgroups
   const long long all = tiles * gz;
   const int rows = (int)std::max<long long>((a.n_q + 65534) / 65535, std::min<long long>(16, a.n_q * all / 2048));
-  hipLaunchKernelGGL((relpos_heads_fwd_kernel<T, V>), dim3((unsigned)tiles, (unsigned)((a.n_q + rows - 1) / rows), gz), dim3(256),
-                     (size_t)heads * a.nb * 4, st, a, heads, rows);
+  rp_dispatch(a.mode, [&](auto m) {
+    hipLaunchKernelGGL((relpos_heads_fwd_kernel<T, V, m.value>), dim3((unsigned)tiles, (unsigned)((a.n_q + rows - 1) / rows), gz), dim3(256),
+                       (size_t)heads * a.nb * 4, st, a, heads, rows);
+  });
 }
 template <typename T> void rp_fwd_run(hipStream_t st, const RpArgs& a, int layout, int v) {
   if (layout == PE_RELPOS_PAIR) {
@@ -292,35 +304,39 @@ template <typename T> void rp_fwd_run(hipStream_t st, const RpArgs& a, int layou
   }
 }
 // Dynamic LDS above 64 KB has to be allowed once per kernel and device
-template <typename K> void allow_lds(K kern) {
-  static std::atomic<unsigned long long> done{0};
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return;      // the launch reports it
-  const unsigned long long bit = 1ull << (dev & 63);
+template <typename K> void allow_lds(K kern, int device, std::atomic<unsigned long long>& done) {
+  const unsigned long long bit = 1ull << (device & 63);
   if (done.load() & bit) return;
-  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 156 * 1024) == hipSuccess) done |= bit;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) done |= bit;
 }
-template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, const RpArgs& a, long long groups) {
+template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
   const int waves = rp_waves(a.nb);
   const long long n = (long long)a.n_q * a.n_k;
-  allow_lds(&relpos_pair_bwd_kernel<T, S, U>);
-  hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, U>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(64 * waves), rp_lds(a.nb, waves), st,
-                     a, (n + groups - 1) / groups);
+  rp_dispatch(a.mode, [&](auto m) {
+    static std::atomic<unsigned long long> done{0};
+    allow_lds(&relpos_pair_bwd_kernel<T, S, U, m.value>, device, done);
+    hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, U, m.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(64 * waves),
+                       rp_lds(a.nb, waves, a.mode), st, a, (n + groups - 1) / groups);
+  });
 }
-template <typename T, int V> void rp_heads_bwd(hipStream_t st, const RpArgs& a, int rows) {
+template <typename T, int V> void rp_heads_bwd(hipStream_t st, int device, const RpArgs& a, int rows) {
+  constexpr int U = V == 8 ? 4 : 8;
   const int waves = rp_waves(a.nb);
-  allow_lds(&relpos_heads_bwd_kernel<T, V>);
-  hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V>), dim3((unsigned)((a.n_k + 64 * V - 1) / (64 * V)), (unsigned)((a.n_q + rows - 1) / rows), (unsigned)a.c),
-                     dim3(64 * waves), rp_lds(a.nb, waves), st, a, rows);
+  rp_dispatch(a.mode, [&](auto m) {
+    static std::atomic<unsigned long long> done{0};
+    allow_lds(&relpos_heads_bwd_kernel<T, V, U, m.value>, device, done);
+    hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, U, m.value>), dim3((unsigned)((a.n_k + 64 * V - 1) / (64 * V)), (unsigned)((a.n_q + rows - 1) / rows), (unsigned)a.c),
+                       dim3(64 * waves), rp_lds(a.nb, waves, a.mode), st, a, rows);
+  });
 }
-template <typename T> void rp_bwd_run(hipStream_t st, const RpArgs& a, int layout, int v, long long groups, int rows) {
+template <typename T> void rp_bwd_run(hipStream_t st, int device, const RpArgs& a, int layout, int v, long long groups, int rows) {
   if (layout == PE_RELPOS_PAIR) {
-    if (a.c > 32) rp_pair_bwd<T, 1, 16>(st, a, groups);
-    else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, a, groups);
-    else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, a, groups);
-    else rp_pair_bwd<T, 8, 8>(st, a, groups);
+    if (a.c > 32) rp_pair_bwd<T, 1, 32>(st, device, a, groups);
+    else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, device, a, groups);
+    else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, device, a, groups);
+    else rp_pair_bwd<T, 8, 8>(st, device, a, groups);
   } else {
-    if (v == 8) rp_heads_bwd<T, 8>(st, a, rows); else if (v == 2) rp_heads_bwd<T, 2>(st, a, rows); else rp_heads_bwd<T, 1>(st, a, rows);
+    if (v == 8) rp_heads_bwd<T, 8>(st, device, a, rows); else if (v == 2) rp_heads_bwd<T, 2>(st, device, a, rows); else rp_heads_bwd<T, 1>(st, device, a, rows);
   }
 }
 
@@ -503,7 +519,7 @@ int pe_relpos_bwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
       groups = pair ? rp_pair_groups(*p) : rp_heads_groups(*p, v);
       const double n = (double)p->n_q * p->n_k * p->c;
       op.launch("relpos bwd", pair ? "relpos_pair_bwd_kernel" : "relpos_heads_bwd_kernel", n, n * e, [&] {
-        if (p->dtype == PE_BF16) rp_bwd_run<bf16>(op.st, a, p->layout, v, groups, rows); else rp_bwd_run<float>(op.st, a, p->layout, v, groups, rows);
+        if (p->dtype == PE_BF16) rp_bwd_run<bf16>(op.st, h->device, a, p->layout, v, groups, rows); else rp_bwd_run<float>(op.st, h->device, a, p->layout, v, groups, rows);
       });
     }
     const int cols = a.nb * p->c;

@@ -10,6 +10,7 @@
 #include "pe_lanes.h"
 
 constexpr int RP_MAX_EDGES = 254;
+constexpr int RP_LUT = 4096;     // widest range of distances with a table of its own
 struct RpArgs {
   const int* pos_q; const int* pos_k; const int* seg_q; const int* seg_k;     // seg_*: null without segments
   const float* table;
@@ -19,80 +20,98 @@ struct RpArgs {
   float* part;
   long long ld;            // elements between rows q
   int n_q, n_k, c, nb;     // nb: buckets, the one of different segments among them
-  int n_edges, dense;      // dense: the edges are consecutive integers
+  int n_edges, mode;       // RpMode
+  int lo, hi;              // DENSE, LUT: first edge - 1, last edge (0, 0 without edges)
   int edges[RP_MAX_EDGES];
 };
+
+// How a bucket is found.  DENSE: the edges are consecutive integers (clipped distances), the clamped distance is the bucket.
+// LUT: the edges span at most RP_LUT distances; a byte per distance in LDS.  SEARCH: any other edges, in LDS, by bisection.  A bisection
+// is up to eight LDS reads that wait for one another: the bias gradient of 16 heads over 2048 x 2048 positions took 400 us with it.
+enum RpMode { RP_DENSE = 0, RP_LUTS = 1, RP_SEARCH = 2 };
+constexpr int rp_lds_words(int mode) { return mode == RP_DENSE ? 1 : mode == RP_LUTS ? RP_LUT / 4 + 1 : RP_MAX_EDGES + 2; }
 
 // Difference of two positions, clamped to 32 bits: no edge is the least 32-bit number, so the clamped value is in the same bucket
 PE_DEV int rp_diff(int a, int b) {
   const long long d = (long long)a - b;
   return (int)(d < -2147483647LL - 1 ? -2147483647LL - 1 : d > 2147483647LL ? 2147483647LL : d);
 }
-// Edges in LDS.  Consecutive edges (clipped distances) need no search.
-struct RpBuckets {
+template <typename E> PE_DEV int rp_search(E&& edge, int n, int d) {
+  int lo = 0, len = n;                                     // edges before lo are <= d, the answer is at most lo + len
+  while (len > 0) {
+    const int half = (len + 1) >> 1;
+    if (edge(lo + half - 1) <= d) lo += half, len -= half; else len = half - 1;
+  }
+  return lo;
+}
+template <int MODE> struct RpBuckets {
   const int* lds;
-  int n, dense, first, other;
+  int n, lo, hi, other;
   // every thread of the workgroup; the caller passes a barrier before the first use
   static PE_DEV void fill(int* lds, const RpArgs& a) {
-    for (int i = threadIdx.x; i < a.n_edges; i += blockDim.x) lds[i] = a.edges[i];
+    if constexpr (MODE == RP_LUTS) {
+      for (int i = threadIdx.x; i <= a.hi - a.lo; i += blockDim.x)
+        reinterpret_cast<uint8_t*>(lds)[i] = (uint8_t)rp_search([&](int k) { return a.edges[k]; }, a.n_edges, a.lo + i);
+    }
+    if constexpr (MODE == RP_SEARCH)
+      for (int i = threadIdx.x; i < a.n_edges; i += blockDim.x) lds[i] = a.edges[i];
   }
-  PE_DEV RpBuckets(const int* l, const RpArgs& a) : lds(l), n(a.n_edges), dense(a.dense), first(a.dense ? a.edges[0] : 0), other(a.nb - 1) {}
+  PE_DEV RpBuckets(const int* l, const RpArgs& a) : lds(l), n(a.n_edges), lo(a.lo), hi(a.hi), other(a.nb - 1) {}
   PE_DEV int of(int pq, int pk) const {
     const int d = rp_diff(pq, pk);
-    if (dense) {
-      if (d < first) return 0;
-      const uint32_t u = (uint32_t)d - (uint32_t)first;      // at least 0: no overflow
-      return u >= (uint32_t)n ? n : (int)u + 1;
-    }
-    int lo = 0, len = n;                                     // edges before lo are <= d
-    while (len > 0) {
-      const int half = (len + 1) >> 1;
-      if (lds[lo + half - 1] <= d) lo += half, len -= half; else len = half - 1;
-    }
-    return lo;
+    if constexpr (MODE == RP_SEARCH) return rp_search([&](int k) { return lds[k]; }, n, d);
+    const int i = min(max(d, lo), hi) - lo;                // 0: below the first edge
+    if constexpr (MODE == RP_LUTS) return reinterpret_cast<const uint8_t*>(lds)[i];
+    return i;
   }
-  PE_DEV int of(int pq, int pk, int sq, int sk) const { return sq != sk ? other : of(pq, pk); }
+  PE_DEV int of(int pq, int pk, int sq, int sk) const {
+    const int b = of(pq, pk);
+    return sq != sk ? other : b;
+  }
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
-// PAIR, forward: a workgroup has one q and RP_PK positions k: first the buckets of those, while `add` is on its way, then
-// V channels per lane and step.
+// PAIR, forward: a workgroup has one q and tile_k positions k.  A lane has V channels of U positions; the positions' numbers and
+// `add` are requested together, then the U table rows, so two round trips to memory lie one behind the other.  Lanes find their
+// buckets each for itself: with buckets passed through LDS two barriers joined the chain (16.8 MB written and read: 21 us).
+// vec_magic: ceil(2^32 / vectors per position), 0 for 1
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V, int U>
-__global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, int tile_k) {
-  __shared__ int edges[RP_MAX_EDGES + 2];
-  __shared__ int bucket[1024];
+template <typename T, int V, int U, int MODE>
+__global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, int tile_k, uint32_t vec_magic) {
+  __shared__ int edges[rp_lds_words(MODE)];
   const int q = blockIdx.y + blockIdx.z * 65535, k0 = blockIdx.x * tile_k;
   if (q >= a.n_q) return;
-  const int nk = min(tile_k, a.n_k - k0), vecs = a.c / V, total = nk * vecs;     // at most 1024 positions
+  const int nk = min(tile_k, a.n_k - k0), vecs = a.c / V, total = nk * vecs;
   const long long base = (long long)q * a.ld + (long long)k0 * a.c;
   const T* add = (const T*)a.add;
   T* out = (T*)a.out;
   Raw<T, V> ad[U];
-  if (add) {
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int e = threadIdx.x + 256 * u;
-      if (e < total) ad[u] = raw_load<T, V>(add + base + (long long)e * V);
-    }
-  }
-  RpBuckets::fill(edges, a);
-  __syncthreads();
-  const RpBuckets rb(edges, a);
-  const int pq = a.pos_q[q], sq = a.seg_q ? a.seg_q[q] : 0;
-  for (int i = threadIdx.x; i < nk; i += 256) bucket[i] = rb.of(pq, a.pos_k[k0 + i], sq, a.seg_q ? a.seg_k[k0 + i] : 0);
-  __syncthreads();
+  int e[U], k[U], pk[U], sk[U];
 #pragma unroll
   for (int u = 0; u < U; u++) {
-    const int e = threadIdx.x + 256 * u;
-    if (e < total) {
-      const int k = e / vecs;
-      const float* t = a.table + (long long)bucket[k] * a.c + (e - k * vecs) * V;
-      Raw<T, V> o;
+    e[u] = min((int)threadIdx.x + 256 * u, total - 1);     // lanes behind the end repeat the last vector
+    k[u] = vec_magic ? (int)__umulhi((uint32_t)e[u], vec_magic) : e[u];
+    pk[u] = a.pos_k[k0 + k[u]];
+    sk[u] = a.seg_q ? a.seg_k[k0 + k[u]] : 0;
+  }
+  if (add)
 #pragma unroll
-      for (int i = 0; i < V; i++) o.set(i, add ? ad[u].get(i) + t[i] : t[i]);
-      raw_store<T, V>(out + base + (long long)e * V, o);
-    }
+    for (int u = 0; u < U; u++) ad[u] = raw_load<T, V>(add + base + (long long)e[u] * V);
+  const int pq = a.pos_q[q], sq = a.seg_q ? a.seg_q[q] : 0;
+  if constexpr (MODE != RP_DENSE) {
+    RpBuckets<MODE>::fill(edges, a);
+    __syncthreads();
+  }
+  const RpBuckets<MODE> rb(edges, a);
+  float t[U][V];
+#pragma unroll
+  for (int u = 0; u < U; u++) load_f32<V>(a.table + (long long)rb.of(pq, pk[u], sq, sk[u]) * a.c + (e[u] - k[u] * vecs) * V, t[u]);
+#pragma unroll
+  for (int u = 0; u < U; u++) {
+    Raw<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; i++) o.set(i, add ? ad[u].get(i) + t[u][i] : t[u][i]);
+    if ((int)threadIdx.x + 256 * u < total) raw_store<T, V>(out + base + (long long)e[u] * V, o);
   }
 }
 
@@ -100,20 +119,20 @@ __global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, in
 // HEADS, forward: a workgroup has one q, 256 V positions k and `heads` heads, whose table columns lie in LDS as [head][bucket]
 // (neighbouring distances are neighbouring banks).  A lane finds its V buckets once for all heads.
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V>
+template <typename T, int V, int MODE>
 __global__ __launch_bounds__(256) void relpos_heads_fwd_kernel(const RpArgs a, int heads, int rows) {
   extern __shared__ float tab[];       // [heads][nb]
-  __shared__ int edges[RP_MAX_EDGES + 2];
+  __shared__ int edges[rp_lds_words(MODE)];
   const int h0 = blockIdx.z * heads, nh = min(heads, a.c - h0);
   const int k = (blockIdx.x * 256 + threadIdx.x) * V;
-  RpBuckets::fill(edges, a);
+  RpBuckets<MODE>::fill(edges, a);
   for (int i = threadIdx.x; i < nh * a.nb; i += 256) {
     const int b = i / nh, h = i - b * nh;
     tab[h * a.nb + b] = a.table[(long long)b * a.c + h0 + h];
   }
   __syncthreads();
   if (k >= a.n_k) return;
-  const RpBuckets rb(edges, a);
+  const RpBuckets<MODE> rb(edges, a);
   int pk[V], sk[V];
 #pragma unroll
   for (int i = 0; i < V; i++) { pk[i] = a.pos_k[k + i]; sk[i] = a.seg_q ? a.seg_k[k + i] : 0; }
@@ -141,58 +160,50 @@ PE_DEV void lds_add(float* p, float v) { __hip_atomic_fetch_add(p, v, __ATOMIC_R
 
 // ---------------------------------------------------------------------------------------------------------------------
 // PAIR, backward.  Lane = channel; a wave walks over positions and adds each to the LDS word [bucket][lane] of its own
-// accumulators.  S positions share a wave where c <= 32.  blockIdx.y: slab of 64 channels (S = 1).
+// accumulators, so that any order of the positions is one LDS operation per 64 elements.  S positions share a wave where c <= 32.
+// blockIdx.y: slab of 64 channels (S = 1).  U loads are in flight per wave; lanes behind the last channel or position load a valid one,
+// since a load under a condition is waited for by itself (2 bytes per lane and 126 us at 384 x 384 x 128).
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int S, int U>
+template <typename T, int S, int U, int MODE>
 __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, long long per_group) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
   constexpr int CL = 64 / S;           // lanes per position
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int sub = lane / CL, ch = blockIdx.y * 64 + lane % CL;
   int* edges = reinterpret_cast<int*>(acc + waves * a.nb * 64);
   float* mine = acc + wave * a.nb * 64 + lane;
-  RpBuckets::fill(edges, a);
+  RpBuckets<MODE>::fill(edges, a);
   for (int i = threadIdx.x; i < waves * a.nb * 64; i += blockDim.x) acc[i] = 0.0f;
   __syncthreads();
-  const RpBuckets rb(edges, a);
-  const T* g = (const T*)a.d_out;
+  const RpBuckets<MODE> rb(edges, a);
+  const T* g = (const T*)a.d_out + min(ch, a.c - 1);
   const long long n = (long long)a.n_q * a.n_k;
   const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
-  const bool on = ch < a.c;
   // a wave takes runs of 64 positions: lane l finds the bucket of the l-th
   for (long long p = p0 + wave * 64; p < p1; p += 64LL * waves) {
     const int cnt = (int)min((long long)64, p1 - p);
     const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
-    int b = 0;
-    long long row = 0;                                                        // this lane's position's offset in d_out
-    if (lane < cnt) {
-      const int over = kk + lane, dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
-      b = rb.of(a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0);
-      row = (long long)q * a.ld + (long long)k * a.c;
-    }
+    const int over = kk + min(lane, cnt - 1), dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
+    const int b = rb.of(a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0);
+    const long long row = (long long)q * a.ld + (long long)k * a.c;            // the position's offset in d_out
     const int rlo = (int)(uint32_t)(uint64_t)row, rhi = (int)(uint32_t)((uint64_t)row >> 32);
 #pragma unroll 1
-    for (int j = 0; j < 64; j += S * U) {
-      if (j >= cnt) break;
-      float v[U];
+    for (int j = 0; j < cnt; j += S * U) {
+      T v[U];
 #pragma unroll
       for (int u = 0; u < U; u++) {
         const int l = j + u * S + sub;
-        long long r;
-        if constexpr (S == 1) {
-          const uint32_t lo = __builtin_amdgcn_readlane(rlo, l), hi = __builtin_amdgcn_readlane(rhi, l);
-          r = (long long)(((uint64_t)hi << 32) | lo);
-        } else {
-          r = (long long)(((uint64_t)(uint32_t)__shfl(rhi, l, 64) << 32) | (uint32_t)__shfl(rlo, l, 64));
-        }
-        v[u] = on && l < cnt ? (float)g[r + ch] : 0.0f;
+        uint32_t lo, hi;
+        if constexpr (S == 1) { lo = __builtin_amdgcn_readlane(rlo, l); hi = __builtin_amdgcn_readlane(rhi, l); }
+        else { lo = (uint32_t)__shfl(rlo, l, 64); hi = (uint32_t)__shfl(rhi, l, 64); }
+        v[u] = g[(long long)(((uint64_t)hi << 32) | lo)];
       }
 #pragma unroll
       for (int u = 0; u < U; u++) {
         const int l = j + u * S + sub;
         int bb;
         if constexpr (S == 1) bb = __builtin_amdgcn_readlane(b, l); else bb = __shfl(b, l, 64);
-        lds_add(mine + bb * 64, v[u]);
+        if (l < cnt) lds_add(mine + bb * 64, (float)v[u]);
       }
     }
   }
@@ -210,19 +221,19 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head and adds each element to the LDS word [bucket][lane]
-// of its own accumulators (bank = lane whatever the buckets are).
+// HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, and adds each element to the LDS word
+// [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V>
+template <typename T, int V, int U, int MODE>
 __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, int rows) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   int* edges = reinterpret_cast<int*>(acc + waves * a.nb * 64);
   float* mine = acc + wave * a.nb * 64 + lane;
-  RpBuckets::fill(edges, a);
+  RpBuckets<MODE>::fill(edges, a);
   for (int i = threadIdx.x; i < waves * a.nb * 64; i += blockDim.x) acc[i] = 0.0f;
   __syncthreads();
-  const RpBuckets rb(edges, a);
+  const RpBuckets<MODE> rb(edges, a);
   const int h = blockIdx.z, k = (blockIdx.x * 64 + lane) * V;
   const int q1 = min(a.n_q, (int)(blockIdx.y + 1) * rows);
   if (k < a.n_k) {
@@ -230,11 +241,21 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, i
 #pragma unroll
     for (int i = 0; i < V; i++) { pk[i] = a.pos_k[k + i]; sk[i] = a.seg_q ? a.seg_k[k + i] : 0; }
     const T* g = (const T*)a.d_out + (long long)h * a.n_q * a.ld + k;
-    for (int q = blockIdx.y * rows + wave; q < q1; q += waves) {
-      const Raw<T, V> v = raw_load<T, V>(g + (long long)q * a.ld);
-      const int pq = a.pos_q[q], sq = a.seg_q ? a.seg_q[q] : 0;
+    for (int q = blockIdx.y * rows + wave; q < q1; q += U * waves) {
+      Raw<T, V> v[U];
 #pragma unroll
-      for (int i = 0; i < V; i++) lds_add(mine + rb.of(pq, pk[i], sq, sk[i]) * 64, v.get(i));
+      for (int u = 0; u < U; u++) v[u] = raw_load<T, V>(g + (long long)min(q + u * waves, q1 - 1) * a.ld);
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int qu = q + u * waves;
+        if (qu >= q1) break;
+        const int pq = a.pos_q[qu], sq = a.seg_q ? a.seg_q[qu] : 0;
+        int b[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) b[i] = rb.of(pq, pk[i], sq, sk[i]);
+#pragma unroll
+        for (int i = 0; i < V; i++) lds_add(mine + b[i] * 64, v[u].get(i));
+      }
     }
   }
   __syncthreads();
