@@ -56,33 +56,41 @@ template <int V> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>& codes)
   return sb;
 }
 
-// One item = V channels of a row; a row has `per_row` items, a multiple of a group's 32 / V, of which those from `n_vec` on hold no
-// channel.  A workgroup takes U runs of 256 consecutive items, all of its loads in flight at once.  HBM-bound.
+// One item = V channels of a row; a row has `per_row` items, a multiple of a group's LG = 32 / V, of which those from `n_vec` on hold no
+// channel, so item / LG numbers the groups.  A wave takes 64 U consecutive items, all of its loads in flight at once; their
+// scales are 64 U / LG consecutive bytes, stored by as many lanes together.  `flat`: no gaps and whole groups, one long row.  HBM-bound.
 template <typename T, int V, int U, bool PACK>
 __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int8_t* codes, uint8_t* scales, T* y, long long rows,
-                                                   int c, int per_row) {
+                                                   int c, int per_row, int flat) {
   constexpr int LG = CK_GROUP / V;
-  const int groups = per_row / LG, n_vec = c / V;
-  const long long first = (long long)blockIdx.x * (256 * U);
-  const long long row0 = first / per_row;
-  const uint32_t rem = (uint32_t)(first - row0 * per_row) + threadIdx.x;
-  long long row[U];
-  int vec[U];
+  const int n_vec = c / V, lane = threadIdx.x & 63;
+  const long long items = rows * per_row, first = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * U);
+  const long long row0 = flat ? 0 : first / per_row;
+  const uint32_t rem = flat ? 0 : (uint32_t)(first - row0 * per_row);
+  long long at[U], code_at[U];       // element offsets in x or y, and in the codes
   bool in[U];
   Raw<T, V> v[U];
   Codes<V> cd[U];
   uint32_t sb[U];
 #pragma unroll
   for (int u = 0; u < U; u++) {
-    const uint32_t off = rem + 256u * u, dr = off / (uint32_t)per_row;
-    row[u] = row0 + dr;
-    vec[u] = (int)(off - dr * (uint32_t)per_row);
-    in[u] = row[u] < rows && vec[u] < n_vec;
+    const long long item = first + 64 * u + lane;
+    if (flat) {
+      in[u] = item < items;
+      at[u] = code_at[u] = item * V;
+    } else {
+      const uint32_t off = rem + 64u * u + lane, dr = off / (uint32_t)per_row;
+      const long long row = row0 + dr;
+      const int vec = (int)(off - dr * (uint32_t)per_row);
+      in[u] = item < items && vec < n_vec;
+      at[u] = row * ld + (long long)vec * V;
+      code_at[u] = row * c + (long long)vec * V;
+    }
     if constexpr (PACK) {
-      v[u] = in[u] ? raw_load<T, V>(x + row[u] * ld + (long long)vec[u] * V) : raw_zero<T, V>();
+      v[u] = in[u] ? raw_load<T, V>(x + at[u]) : raw_zero<T, V>();
     } else if (in[u]) {
-      cd[u] = *reinterpret_cast<const Codes<V>*>(codes + row[u] * c + (long long)vec[u] * V);
-      sb[u] = scales[row[u] * groups + vec[u] / LG];
+      cd[u] = *reinterpret_cast<const Codes<V>*>(codes + code_at[u]);
+      sb[u] = scales[item / LG];
     }
   }
 #pragma unroll
@@ -91,16 +99,25 @@ __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int
       float f[V];
 #pragma unroll
       for (int i = 0; i < V; i++) f[i] = v[u].get(i);
-      const uint32_t s = ck_encode<V>(f, cd[u]);
-      if (in[u]) {
-        *reinterpret_cast<Codes<V>*>(codes + row[u] * c + (long long)vec[u] * V) = cd[u];
-        if (vec[u] % LG == 0) scales[row[u] * groups + vec[u] / LG] = (uint8_t)s;
-      }
+      sb[u] = ck_encode<V>(f, cd[u]);
+      if (in[u]) *reinterpret_cast<Codes<V>*>(codes + code_at[u]) = cd[u];
     } else if (in[u]) {
       const float s = ck_scale(sb[u]);
 #pragma unroll
       for (int i = 0; i < V; i++) v[u].set(i, (float)cd[u].get(i) * s);
-      raw_store<T, V>(y + row[u] * ld + (long long)vec[u] * V, v[u]);
+      raw_store<T, V>(y + at[u], v[u]);
     }
+  }
+  if constexpr (PACK) {
+    constexpr int PER = 64 / LG, N = U * PER;      // groups per 64 items, per wave
+    static_assert(N <= 64, "a lane stores one scale");
+    uint32_t mine = 0;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const uint32_t s = (uint32_t)__shfl((int)sb[u], (lane % PER) * LG, 64);
+      if (lane / PER == u) mine = s;
+    }
+    const long long group = first / LG + lane;
+    if (lane < N && group < items / LG) scales[group] = (uint8_t)mine;
   }
 }

@@ -43,6 +43,20 @@ template <int L> PE_DEV float row_sum(float v, float* red) {
   return v;
 }
 
+// two sums at once, with one barrier
+template <int L> PE_DEV void row_sums(float& p, float& q, float* red, float* red2) {
+  p = lanes_sum<(L < 64 ? L : 64)>(p);
+  q = lanes_sum<(L < 64 ? L : 64)>(q);
+  if constexpr (L > 64) {
+    constexpr int W = L / 64;
+    if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = p; red2[threadIdx.x >> 6] = q; }
+    __syncthreads();
+    p = q = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; w++) { p += red[w]; q += red2[w]; }
+  }
+}
+
 // Workgroup shape of a row of L lanes: rows side by side
 template <int L> struct LnShape {
   static constexpr int THREADS = L > 256 ? L : 256;
@@ -218,7 +232,8 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
         s2 += u * z;
       }
     if (dx) {
-      const float m1 = row_sum<L>(s1, red[slot]) * inv_c, m2 = row_sum<L>(s2, red[slot + 1]) * inv_c;
+      row_sums<L>(s1, s2, red[slot], red[slot + 1]);
+      const float m1 = s1 * inv_c, m2 = s2 * inv_c;
 #pragma unroll
       for (int n = 0; n < NV; n++) {
         Raw<T, V> o;

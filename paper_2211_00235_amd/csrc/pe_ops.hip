@@ -95,7 +95,7 @@ void ck_launch(hipStream_t st, const void* x, long long ld, void* ckpt, void* y,
   const int per_row = (int)ck_groups(c) * (CK_GROUP / V);
   const long long items = rows * per_row, blocks = (items + 256 * U - 1) / (256 * U);
   hipLaunchKernelGGL((ckpt_kernel<T, V, U, PACK>), dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
-                     (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row);
+                     (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row, (int)(c % CK_GROUP == 0 && (ld == c || rows == 1)));
 }
 template <bool PACK> void ck_run(hipStream_t st, int dtype, int v, const void* x, long long ld, void* ckpt, void* y, long long rows, int c) {
   if (dtype == PE_BF16) {

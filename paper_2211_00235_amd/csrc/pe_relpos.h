@@ -154,13 +154,14 @@ __global__ __launch_bounds__(256) void relpos_heads_fwd_kernel(const RpArgs a, i
   }
 }
 
-// v is added to an LDS word that belongs to this lane alone (LDS operations of a wave execute in order, so the sum's order is
-// the program's): one instruction without a result to wait for
-PE_DEV void lds_add(float* p, float v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+// v is added to an LDS word that belongs to this lane alone, by a read and a write: the LDS operations of a wave execute in order, so
+// the sum's order is the program's.  An LDS atomic took 200 cycles of a CU per 64 lanes (heads 2048 x 2048 x 16: 341 us).
+PE_DEV void lds_add(float* p, float v) { *p += v; }
 
 // ---------------------------------------------------------------------------------------------------------------------
 // PAIR, backward.  Lane = channel; a wave walks over positions and adds each to the LDS word [bucket][lane] of its own
-// accumulators, so that any order of the positions is one LDS operation per 64 elements.  S positions share a wave where c <= 32.
+// accumulators.  Neighbouring positions of the same bucket (all that are farther than the outermost edges) are added in a register
+// first, which the whole wave decides together where it has one position at a time.  S positions share a wave where c <= 32.
 // blockIdx.y: slab of 64 channels (S = 1).  U loads are in flight per wave; lanes behind the last channel or position load a valid one,
 // since a load under a condition is waited for by itself (2 bytes per lane and 126 us at 384 x 384 x 128).
 // ---------------------------------------------------------------------------------------------------------------------
@@ -186,6 +187,8 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
     const int over = kk + min(lane, cnt - 1), dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
     const int b = rb.of(a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0);
     const long long row = (long long)q * a.ld + (long long)k * a.c;            // the position's offset in d_out
+    int run = S == 1 ? __builtin_amdgcn_readlane(b, 0) : 0;                   // bucket of the run that is being added up
+    float sum = 0.0f;
     const int rlo = (int)(uint32_t)(uint64_t)row, rhi = (int)(uint32_t)((uint64_t)row >> 32);
 #pragma unroll 1
     for (int j = 0; j < cnt; j += S * U) {
@@ -201,11 +204,19 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 #pragma unroll
       for (int u = 0; u < U; u++) {
         const int l = j + u * S + sub;
-        int bb;
-        if constexpr (S == 1) bb = __builtin_amdgcn_readlane(b, l); else bb = __shfl(b, l, 64);
-        if (l < cnt) lds_add(mine + bb * 64, (float)v[u]);
+        if constexpr (S == 1) {
+          const int bb = __builtin_amdgcn_readlane(b, l);
+          if (l < cnt) {
+            if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
+            sum += (float)v[u];
+          }
+        } else {
+          const int bb = __shfl(b, l, 64);
+          if (l < cnt) lds_add(mine + bb * 64, (float)v[u]);
+        }
       }
     }
+    if constexpr (S == 1) lds_add(mine + run * 64, sum);
   }
   __syncthreads();
   // the waves' accumulators and the positions side by side, in a fixed order
@@ -222,7 +233,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 
 // ---------------------------------------------------------------------------------------------------------------------
 // HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, and adds each element to the LDS word
-// [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).
+// [bucket][lane] of its own accumulators (bank = lane whatever the buckets are); V elements of the same bucket are added up first.
 // ---------------------------------------------------------------------------------------------------------------------
 template <typename T, int V, int U, int MODE>
 __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, int rows) {
@@ -253,8 +264,14 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, i
         int b[V];
 #pragma unroll
         for (int i = 0; i < V; i++) b[i] = rb.of(pq, pk[i], sq, sk[i]);
+        bool same = true;
+        float sum = v[u].get(0);
 #pragma unroll
-        for (int i = 0; i < V; i++) lds_add(mine + b[i] * 64, v[u].get(i));
+        for (int i = 1; i < V; i++) { same = same && b[i] == b[0]; sum += v[u].get(i); }
+        if (same) lds_add(mine + b[0] * 64, sum);
+        else
+#pragma unroll
+          for (int i = 0; i < V; i++) lds_add(mine + b[i] * 64, v[u].get(i));
       }
     }
   }
