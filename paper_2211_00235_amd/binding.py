@@ -168,6 +168,7 @@ class Handle:
         rc = lib().pe_create(C.byref(self._h))
         if rc:
             raise PEError("pe_create: " + strerror(rc))
+        self.device = int(lib().pe_handle_device(self._h))      # index of the device that was current
 
     def set_option(self, opt, value):
         rc = lib().pe_set_option(self._h, opt, value)
@@ -185,14 +186,6 @@ class Handle:
             raise PEError(strerror(n))
         return [dict(name=e.name.decode(), kernel=e.kernel.decode(), launches=int(e.launches), total_ms=float(e.total_ms),
                      flops=float(e.flops), bytes=float(e.bytes)) for e in arr[:n]]
-
-    @property
-    def device(self):
-        """Index of the device that was current when the handle was made."""
-        d = self.__dict__.get("_device")
-        if d is None:
-            d = self._device = int(lib().pe_handle_device(self._h))
-        return d
 
     def last_error(self):
         return lib().pe_last_error(self._h).decode()
@@ -275,10 +268,10 @@ def stack_fwd_bwd(h, n_extra, extra, n_main, main, extra_msa_in, msa_in, pair_in
 # Operators around the trunk (include/pe.h says what they compute).  Tensors are torch tensors on the handle's device; a
 # tensor [..., c] counts as rows of c channels, with gaps between the rows only where it has two dimensions.
 # ---------------------------------------------------------------------------
-_DTYPES = {}
+_DTYPES = {}      # by torch type, filled as types come
 
 
-def _dtype(t, what):
+def _dtype(t):
     d = _DTYPES.get(t.dtype)
     if d is None:
         d = _DTYPES[t.dtype] = {"torch.float32": PE_F32, "torch.bfloat16": PE_BF16, "torch.uint8": PE_CKPT,
@@ -287,24 +280,27 @@ def _dtype(t, what):
 
 
 def _on(h, t, what):
-    if not t.is_cuda or t.get_device() != h.device:
+    if t.get_device() != h.device:      # -1: host memory
         raise PEError("%s: not on the handle's device" % what)
 
 
 def _rows(h, t, what, like=None):
     """(type, rows, c, row stride) of a tensor of activations; `like`: what another one has to agree with."""
-    _on(h, t, what)
-    d, shape = _dtype(t, what), t.shape
-    if d not in (PE_F32, PE_BF16) or not shape:
+    if t.get_device() != h.device:
+        _on(h, t, what)
+    d, shape = _DTYPES.get(t.dtype), t.shape
+    if d is None:
+        d = _dtype(t)
+    if (d != PE_F32 and d != PE_BF16) or not shape:
         raise PEError("%s: a float32 or bfloat16 tensor [..., c] is wanted" % what)
     c = shape[-1]
-    if len(shape) == 2 and (c == 1 or t.stride(1) == 1):
-        rows, ld = shape[0], (t.stride(0) if shape[0] > 1 else c)
-    elif t.is_contiguous():
+    if t.is_contiguous():
         rows, ld = (t.numel() // c if c else 0), c
+    elif len(shape) == 2 and (c == 1 or t.stride(1) == 1):
+        rows, ld = shape[0], (t.stride(0) if shape[0] > 1 else c)
     else:
         raise PEError("%s: channels have to be neighbours in memory, rows of a tensor with more than two dimensions too" % what)
-    if like is not None and like != (d, rows, c):
+    if like is not None and (d, rows, c) != like:
         raise PEError("%s: shape or type differs" % what)
     return d, rows, c, ld
 
@@ -313,8 +309,9 @@ def _vec(h, t, n, what, dtype=PE_F32):
     """Device pointer of a contiguous tensor of n elements (None: NULL)."""
     if t is None:
         return None
-    _on(h, t, what)
-    if _dtype(t, what) != dtype or t.numel() != n or not t.is_contiguous():
+    if t.get_device() != h.device:
+        _on(h, t, what)
+    if _dtype(t) != dtype or t.numel() != n or not t.is_contiguous():
         raise PEError("%s: a contiguous tensor of %d elements is wanted" % (what, n))
     return t.data_ptr()
 
@@ -323,7 +320,7 @@ def _bytes(h, t, n, what):
     if t is None:
         return None
     _on(h, t, what)
-    if not t.is_contiguous() or t.numel() * t.element_size() < n:
+    if not t.is_contiguous() or t.nbytes < n:
         raise PEError("%s: %d contiguous bytes are wanted" % (what, n))
     return t.data_ptr()
 
@@ -354,14 +351,14 @@ def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=No
     not wanted."""
     d, rows, c, ldy = _rows(h, dy, "dy")
     like = (d, rows, c)
-    kept = _dtype(x, "x") == PE_CKPT
+    kept = _dtype(x) == PE_CKPT
     if kept:
         px, ldx = _bytes(h, x, ckpt_bytes(rows, c), "x"), 0
     else:
         ldx, px = _rows(h, x, "x", like)[3], x.data_ptr()
     lda = _rows(h, add, "add", like)[3] if add is not None else 0
     ldd = _rows(h, dx, "dx", like)[3] if dx is not None else 0
-    ws = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws = 0 if workspace is None else workspace.nbytes
     _op(h, lib().pe_layernorm_bwd(
         h._h, rows, c, d, PE_CKPT if kept else d, px, ldx, _vec(h, stats, 2 * rows, "stats"), _vec(h, gain, c, "gain"),
         dy.data_ptr(), ldy, None if add is None else add.data_ptr(), lda, None if dx is None else dx.data_ptr(), ldd,
@@ -397,10 +394,10 @@ def _relpos(h, pos_q, pos_k, edges, t, seg_q, seg_k, layout, what):
         raise PEError("layout: 'pair' or 'heads'")
     if (seg_q is None) != (seg_k is None):
         raise PEError("segments: seg_q and seg_k belong together")
-    if edges.is_cuda or _dtype(edges, "edges") != "int32" or not edges.is_contiguous():
+    if edges.is_cuda or _dtype(edges) != "int32" or not edges.is_contiguous():
         raise PEError("edges: a contiguous int32 tensor in host memory is wanted")
     n_q, n_k = pos_q.numel(), pos_k.numel()
-    pair, d = layout == "pair", _dtype(t, what)
+    pair, d = layout == "pair", _dtype(t)
     if d not in (PE_F32, PE_BF16) or t.dim() != 3:
         raise PEError("%s: a float32 or bfloat16 tensor of three dimensions is wanted" % what)
     s, st = t.shape, t.stride()
@@ -441,5 +438,5 @@ def relpos_bwd(h, pos_q, pos_k, edges, d_out, d_table, workspace, seg_q=None, se
     """d_table [buckets, c] = sum of d_out over the pairs of each bucket."""
     p, ptr, n = _relpos(h, pos_q, pos_k, edges, d_out, seg_q, seg_k, layout, "d_out")
     _op(h, lib().pe_relpos_bwd(h._h, C.byref(p), *ptr, d_out.data_ptr(), _vec(h, d_table, n, "d_table"), int(accumulate),
-                               _bytes(h, workspace, 0, "workspace"), workspace.numel() * workspace.element_size(), _s(stream)),
+                               _bytes(h, workspace, 0, "workspace"), workspace.nbytes, _s(stream)),
         "pe_relpos_bwd")

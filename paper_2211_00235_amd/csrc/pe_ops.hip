@@ -155,10 +155,13 @@ LnPlan ln_plan(int c, int v) {
   if (n <= 4096) return {1024, 4};
   return v == 2 ? LnPlan{1024, 8} : LnPlan{1024, 16};
 }
+// Most workgroups of a launch: they walk over the rows.  Backward, each writes 8 c bytes of partial sums: as many as the chip holds at once,
+// four per CU of rows within waves, two or one of rows of whole workgroups (4096 x 8192 with 512 of them 60 us and 11 for the sums,
+// with 256 49 and 7).
 constexpr int LN_FWD_WG = 2048, LN_BWD_WG = 1024;
 long long ln_bwd_groups(long long rows, int c, int v) {
   const LnPlan p = ln_plan(c, v);
-  return std::min<long long>((rows + p.rows() - 1) / p.rows(), p.l <= 64 ? LN_BWD_WG : 512);
+  return std::min<long long>((rows + p.rows() - 1) / p.rows(), p.l <= 64 ? LN_BWD_WG : p.l == 256 ? 512 : 256);
 }
 
 template <typename T, int V, int L, int NV> void ln_fwd_launch(hipStream_t st, const LnArgs& a) {
@@ -251,7 +254,7 @@ int rp_check(OpCall& op, const pe_relpos* p, const int* edges, const int* pos_q,
     a.edges[i] = edges[i];
   }
   a.lo = p->n_edges ? edges[0] - 1 : 0;
-  a.hi = p->n_edges ? edges[p->n_edges - 1] : 0;
+  a.hi = p->n_edges ? edges[p->n_edges - 1] : 0;        // without edges both are 0: every distance is in bucket 0
   a.mode = dense ? RP_DENSE : (long long)a.hi - a.lo < RP_LUT ? RP_LUTS : RP_SEARCH;
   const bool some = p->n_q > 0 && p->n_k > 0;
   if (some && (!pos_q || !pos_k || (p->segments && (!seg_q || !seg_k)))) return op.refuse(PE_ERR_NULL, "relative positions: null positions or segments");
@@ -331,7 +334,7 @@ template <typename T, int V> void rp_heads_bwd(hipStream_t st, int device, const
 }
 template <typename T> void rp_bwd_run(hipStream_t st, int device, const RpArgs& a, int layout, int v, long long groups, int rows) {
   if (layout == PE_RELPOS_PAIR) {
-    if (a.c > 32) rp_pair_bwd<T, 1, 32>(st, device, a, groups);
+    if (a.c > 32) rp_pair_bwd<T, 1, 64>(st, device, a, groups);
     else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, device, a, groups);
     else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, device, a, groups);
     else rp_pair_bwd<T, 8, 8>(st, device, a, groups);

@@ -70,6 +70,29 @@ template <int MODE> struct RpBuckets {
   }
 };
 
+// V neighbouring positions k of a lane.  far(): the bucket of all of them against q where it can be told without a look at each (all
+// beyond the outermost edges, or all of one other segment), otherwise -1.
+template <int V> struct RpLane {
+  int pos[V], seg[V], least, most;
+  bool one_seg;
+  PE_DEV RpLane(const RpArgs& a, int k) {
+#pragma unroll
+    for (int i = 0; i < V; i++) { pos[i] = a.pos_k[k + i]; seg[i] = a.seg_q ? a.seg_k[k + i] : 0; }
+    least = most = pos[0];
+    one_seg = true;
+#pragma unroll
+    for (int i = 1; i < V; i++) { least = min(least, pos[i]); most = max(most, pos[i]); one_seg = one_seg && seg[i] == seg[0]; }
+  }
+  template <int MODE> PE_DEV int far(const RpBuckets<MODE>& rb, int pq, int sq) const {
+    if constexpr (V == 1) return rb.of(pq, pos[0], sq, seg[0]);
+    if (!one_seg) return -1;
+    if (sq != seg[0]) return rb.other;
+    if (rp_diff(pq, least) <= rb.lo) return 0;            // the largest distance is below the first edge
+    if (rp_diff(pq, most) >= rb.hi) return rb.n;
+    return -1;
+  }
+};
+
 // ---------------------------------------------------------------------------------------------------------------------
 // PAIR, forward: a workgroup has one q and tile_k positions k.  A lane has V channels of U positions; the positions' numbers and
 // `add` are requested together, then the U table rows, so two round trips to memory lie one behind the other.  Lanes find their
@@ -133,23 +156,36 @@ __global__ __launch_bounds__(256) void relpos_heads_fwd_kernel(const RpArgs a, i
   __syncthreads();
   if (k >= a.n_k) return;
   const RpBuckets<MODE> rb(edges, a);
-  int pk[V], sk[V];
-#pragma unroll
-  for (int i = 0; i < V; i++) { pk[i] = a.pos_k[k + i]; sk[i] = a.seg_q ? a.seg_k[k + i] : 0; }
+  const RpLane<V> at(a, k);
   const T* add = (const T*)a.add;
   T* out = (T*)a.out;
   for (int q = blockIdx.y * rows; q < min(a.n_q, (int)(blockIdx.y + 1) * rows); q++) {
-    const int pq = a.pos_q[q], sq = a.seg_q ? a.seg_q[q] : 0;
+    const int pq = a.pos_q[q], sq = a.seg_q ? a.seg_q[q] : 0, far = at.far(rb, pq, sq);
     int b[V];
+    if (far >= 0) {
 #pragma unroll
-    for (int i = 0; i < V; i++) b[i] = rb.of(pq, pk[i], sq, sk[i]);
+      for (int i = 0; i < V; i++) b[i] = far;
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; i++) b[i] = rb.of(pq, at.pos[i], sq, at.seg[i]);
+    }
+    const bool all_far = V > 1 && __all(far >= 0);       // of the wave: one table entry per lane and head
     for (int h = 0; h < nh; h++) {
-      const long long at = ((long long)(h0 + h) * a.n_q + q) * a.ld + k;
+      const long long o_at = ((long long)(h0 + h) * a.n_q + q) * a.ld + k;
       Raw<T, V> o, ad;
-      if (add) ad = raw_load<T, V>(add + at);
+      if (add) ad = raw_load<T, V>(add + o_at);
+      float t[V];
+      if (all_far) {
+        const float one = tab[h * a.nb + far];
 #pragma unroll
-      for (int i = 0; i < V; i++) o.set(i, add ? ad.get(i) + tab[h * a.nb + b[i]] : tab[h * a.nb + b[i]]);
-      raw_store<T, V>(out + at, o);
+        for (int i = 0; i < V; i++) t[i] = one;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) t[i] = tab[h * a.nb + b[i]];
+      }
+#pragma unroll
+      for (int i = 0; i < V; i++) o.set(i, add ? ad.get(i) + t[i] : t[i]);
+      raw_store<T, V>(out + o_at, o);
     }
   }
 }
@@ -173,34 +209,48 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
   const int sub = lane / CL, ch = blockIdx.y * 64 + lane % CL;
   int* edges = reinterpret_cast<int*>(acc + waves * a.nb * 64);
   float* mine = acc + wave * a.nb * 64 + lane;
+  const T* g = (const T*)a.d_out + min(ch, a.c - 1);
+  const long long n = (long long)a.n_q * a.n_k;
+  const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
+  // a wave takes runs of 64 positions: lane l finds the place and the distance of the l-th
+  int cnt, pq, pk, sq, sk, rlo, rhi;
+  auto locate = [&](long long p) {
+    cnt = (int)min((long long)64, p1 - p);
+    const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
+    const int over = kk + min(lane, cnt - 1), dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
+    pq = a.pos_q[q];
+    pk = a.pos_k[k];
+    sq = a.seg_q ? a.seg_q[q] : 0;
+    sk = a.seg_q ? a.seg_k[k] : 0;
+    const long long row = (long long)q * a.ld + (long long)k * a.c;            // the position's offset in d_out
+    rlo = (int)(uint32_t)(uint64_t)row;
+    rhi = (int)(uint32_t)((uint64_t)row >> 32);
+  };
+  T v[U];
+  auto load = [&](int j) {
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int l = j + u * S + sub;
+      uint32_t lo, hi;
+      if constexpr (S == 1) { lo = __builtin_amdgcn_readlane(rlo, l); hi = __builtin_amdgcn_readlane(rhi, l); }
+      else { lo = (uint32_t)__shfl(rlo, l, 64); hi = (uint32_t)__shfl(rhi, l, 64); }
+      v[u] = g[(long long)(((uint64_t)hi << 32) | lo)];
+    }
+  };
+  long long p = p0 + wave * 64;
+  if (p < p1) { locate(p); load(0); }      // on their way while the accumulators are cleared
   RpBuckets<MODE>::fill(edges, a);
   for (int i = threadIdx.x; i < waves * a.nb * 64; i += blockDim.x) acc[i] = 0.0f;
   __syncthreads();
   const RpBuckets<MODE> rb(edges, a);
-  const T* g = (const T*)a.d_out + min(ch, a.c - 1);
-  const long long n = (long long)a.n_q * a.n_k;
-  const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
-  // a wave takes runs of 64 positions: lane l finds the bucket of the l-th
-  for (long long p = p0 + wave * 64; p < p1; p += 64LL * waves) {
-    const int cnt = (int)min((long long)64, p1 - p);
-    const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
-    const int over = kk + min(lane, cnt - 1), dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
-    const int b = rb.of(a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0);
-    const long long row = (long long)q * a.ld + (long long)k * a.c;            // the position's offset in d_out
-    int run = S == 1 ? __builtin_amdgcn_readlane(b, 0) : 0;                   // bucket of the run that is being added up
+  for (bool first = true; p < p1; p += 64LL * waves, first = false) {
+    if (!first) { locate(p); load(0); }
+    const int b = rb.of(pq, pk, sq, sk);
+    int run = S == 1 ? __builtin_amdgcn_readlane(b, 0) : 0;                    // bucket of the run that is being added up
     float sum = 0.0f;
-    const int rlo = (int)(uint32_t)(uint64_t)row, rhi = (int)(uint32_t)((uint64_t)row >> 32);
 #pragma unroll 1
     for (int j = 0; j < cnt; j += S * U) {
-      T v[U];
-#pragma unroll
-      for (int u = 0; u < U; u++) {
-        const int l = j + u * S + sub;
-        uint32_t lo, hi;
-        if constexpr (S == 1) { lo = __builtin_amdgcn_readlane(rlo, l); hi = __builtin_amdgcn_readlane(rhi, l); }
-        else { lo = (uint32_t)__shfl(rlo, l, 64); hi = (uint32_t)__shfl(rhi, l, 64); }
-        v[u] = g[(long long)(((uint64_t)hi << 32) | lo)];
-      }
+      if (j) load(j);
 #pragma unroll
       for (int u = 0; u < U; u++) {
         const int l = j + u * S + sub;
@@ -232,8 +282,9 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, and adds each element to the LDS word
-// [bucket][lane] of its own accumulators (bank = lane whatever the buckets are); V elements of the same bucket are added up first.
+// HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, and adds to the LDS words
+// [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).  Most lanes' positions are all farther than the outermost
+// edges, which their extremes tell: V elements are then one addition to LDS and no bucket is looked up.
 // ---------------------------------------------------------------------------------------------------------------------
 template <typename T, int V, int U, int MODE>
 __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, int rows) {
@@ -248,30 +299,38 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, i
   const int h = blockIdx.z, k = (blockIdx.x * 64 + lane) * V;
   const int q1 = min(a.n_q, (int)(blockIdx.y + 1) * rows);
   if (k < a.n_k) {
-    int pk[V], sk[V];
-#pragma unroll
-    for (int i = 0; i < V; i++) { pk[i] = a.pos_k[k + i]; sk[i] = a.seg_q ? a.seg_k[k + i] : 0; }
+    RpLane<V> at(a, k);
     const T* g = (const T*)a.d_out + (long long)h * a.n_q * a.ld + k;
-    for (int q = blockIdx.y * rows + wave; q < q1; q += U * waves) {
+    Raw<T, V> next[U];
+    auto fetch = [&](int q) {
+#pragma unroll
+      for (int u = 0; u < U; u++) next[u] = raw_load<T, V>(g + (long long)min(q + u * waves, q1 - 1) * a.ld);
+    };
+    int q = blockIdx.y * rows + wave;
+    if (q < q1) fetch(q);
+    for (; q < q1; q += U * waves) {
       Raw<T, V> v[U];
 #pragma unroll
-      for (int u = 0; u < U; u++) v[u] = raw_load<T, V>(g + (long long)min(q + u * waves, q1 - 1) * a.ld);
+      for (int u = 0; u < U; u++) v[u] = next[u];
+      if (q + U * waves < q1) fetch(q + U * waves);
 #pragma unroll
       for (int u = 0; u < U; u++) {
         const int qu = q + u * waves;
         if (qu >= q1) break;
         const int pq = a.pos_q[qu], sq = a.seg_q ? a.seg_q[qu] : 0;
-        int b[V];
+        const int far = at.far(rb, pq, sq);
+        if (far >= 0) {
+          float sum = v[u].get(0);
 #pragma unroll
-        for (int i = 0; i < V; i++) b[i] = rb.of(pq, pk[i], sq, sk[i]);
-        bool same = true;
-        float sum = v[u].get(0);
+          for (int i = 1; i < V; i++) sum += v[u].get(i);
+          lds_add(mine + far * 64, sum);
+        } else {
+          int b[V];
 #pragma unroll
-        for (int i = 1; i < V; i++) { same = same && b[i] == b[0]; sum += v[u].get(i); }
-        if (same) lds_add(mine + b[0] * 64, sum);
-        else
+          for (int i = 0; i < V; i++) b[i] = rb.of(pq, at.pos[i], sq, at.seg[i]);
 #pragma unroll
           for (int i = 0; i < V; i++) lds_add(mine + b[i] * 64, v[u].get(i));
+        }
       }
     }
   }
