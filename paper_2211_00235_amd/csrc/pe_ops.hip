@@ -223,17 +223,12 @@ long long rp_pair_groups(const pe_relpos& p) {
   const long long n = (long long)p.n_q * p.n_k;
   return std::max<long long>(1, std::min<long long>(128, (n + 511) / 512));
 }
-// HEADS: rows q per workgroup, so that about 512 workgroups share the work
-int rp_heads_rows(const pe_relpos& p, int v) {
+// HEADS: workgroups that share the rows q of a head and 64 v positions k, so that about 512 share the work, with a row per wave at least
+int rp_heads_split(const pe_relpos& p, int v) {
   const long long tiles = (p.n_k + 64LL * v - 1) / (64LL * v) * p.c;
-  const long long split = std::max<long long>(1, (512 + tiles - 1) / tiles);
-  const long long least = 8;      // a row for each wave
-  return (int)std::max<long long>(least, (p.n_q + split - 1) / split);
+  return (int)std::min<long long>((p.n_q + 7) / 8, std::max<long long>(1, (512 + tiles - 1) / tiles));
 }
-long long rp_heads_groups(const pe_relpos& p, int v) {
-  const int rows = rp_heads_rows(p, v);
-  return (long long)((p.n_k + 64 * v - 1) / (64 * v)) * ((p.n_q + rows - 1) / rows);
-}
+long long rp_heads_groups(const pe_relpos& p, int v) { return (long long)((p.n_k + 64 * v - 1) / (64 * v)) * rp_heads_split(p, v); }
 size_t rp_workspace(const pe_relpos& p) {
   if (p.n_q == 0 || p.n_k == 0) return 256;
   const long long g = p.layout == PE_RELPOS_PAIR ? rp_pair_groups(p)
@@ -271,11 +266,15 @@ size_t rp_span(const pe_relpos& p) {
                                     : span((long long)p.n_q * p.c, rp_row(p), rp_ld(p), elem(p.dtype));
 }
 
-// calls `f` with the mode as a template argument
-template <typename F> void rp_dispatch(int mode, F&& f) {
+// calls `f` with the mode as a template argument; few: a lane looks up fewer than ten distances
+template <typename F> void rp_dispatch(int mode, bool few, F&& f) {
   if (mode == RP_DENSE) f(std::integral_constant<int, RP_DENSE>{});
-  else if (mode == RP_LUTS) f(std::integral_constant<int, RP_LUTS>{});
+  else if (mode == RP_LUTS && !few) f(std::integral_constant<int, RP_LUTS>{});
   else f(std::integral_constant<int, RP_SEARCH>{});
+}
+// the same for kernels whose lanes always look up few
+template <typename F> void rp_dispatch_few(int mode, F&& f) {
+  if (mode == RP_DENSE) f(std::integral_constant<int, RP_DENSE>{}); else f(std::integral_constant<int, RP_SEARCH>{});
 }
 template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
   constexpr int U = V == 8 ? 4 : 8;
@@ -283,7 +282,7 @@ template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
   const int tile = std::max(1, 256 * U / vecs);          // vecs <= 1024 <= 256 U (c <= 1024): at least one position
   const unsigned magic = vecs == 1 ? 0u : (unsigned)(((1ull << 32) + vecs - 1) / vecs);     // exact for vectors up to 2^11
   const unsigned gx = (unsigned)((a.n_k + tile - 1) / tile), gy = (unsigned)std::min(a.n_q, 65535), gz = (unsigned)((a.n_q + 65534) / 65535);
-  rp_dispatch(a.mode, [&](auto m) { hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U, m.value>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile, magic); });
+  rp_dispatch_few(a.mode, [&](auto m) { hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U, m.value>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile, magic); });
 }
 template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) {
   // heads per workgroup: what 32 KB of LDS hold, and few enough that the chip is filled
@@ -291,10 +290,10 @@ template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) 
   int heads = std::max(1, std::min(a.c, 32 * 1024 / (a.nb * 4)));
   while (heads > 1 && tiles * a.n_q * ((a.c + heads - 1) / heads) < 512) heads = (heads + 1) / 2;
   const unsigned gz = (unsigned)((a.c + heads - 1) / heads);
-  // rows per workgroup: the table's copy in LDS is shared by as many rows as leave 2048 workgroups
+  // rows per workgroup: the table's copy in LDS is shared by as many rows as leave 512 workgroups
   const long long all = tiles * gz;
-  const int rows = (int)std::max<long long>((a.n_q + 65534) / 65535, std::min<long long>(16, a.n_q * all / 2048));
-  rp_dispatch(a.mode, [&](auto m) {
+  const int rows = (int)std::max<long long>((a.n_q + 65534) / 65535, std::min<long long>(16, a.n_q * all / 512));
+  rp_dispatch(a.mode, rows * V < 10, [&](auto m) {
     hipLaunchKernelGGL((relpos_heads_fwd_kernel<T, V, m.value>), dim3((unsigned)tiles, (unsigned)((a.n_q + rows - 1) / rows), gz), dim3(256),
                        (size_t)heads * a.nb * 4, st, a, heads, rows);
   });
@@ -312,34 +311,34 @@ template <typename K> void allow_lds(K kern, int device, std::atomic<unsigned lo
   if (done.load() & bit) return;
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) done |= bit;
 }
-template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
+template <typename T, int S> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
   const int waves = rp_waves(a.nb);
   const long long n = (long long)a.n_q * a.n_k;
-  rp_dispatch(a.mode, [&](auto m) {
+  rp_dispatch_few(a.mode, [&](auto m) {
     static std::atomic<unsigned long long> done{0};
-    allow_lds(&relpos_pair_bwd_kernel<T, S, U, m.value>, device, done);
-    hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, U, m.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(64 * waves),
-                       rp_lds(a.nb, waves, a.mode), st, a, (n + groups - 1) / groups);
+    allow_lds(&relpos_pair_bwd_kernel<T, S, m.value>, device, done);
+    hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, m.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(64 * waves),
+                       rp_lds(a.nb, waves, m.value), st, a, (n + groups - 1) / groups);
   });
 }
-template <typename T, int V> void rp_heads_bwd(hipStream_t st, int device, const RpArgs& a, int rows) {
+template <typename T, int V> void rp_heads_bwd(hipStream_t st, int device, const RpArgs& a, int split) {
   constexpr int U = V == 8 ? 4 : 8;
   const int waves = rp_waves(a.nb);
-  rp_dispatch(a.mode, [&](auto m) {
+  rp_dispatch(a.mode, (long long)V * a.n_q < 10LL * split * waves, [&](auto m) {
     static std::atomic<unsigned long long> done{0};
     allow_lds(&relpos_heads_bwd_kernel<T, V, U, m.value>, device, done);
-    hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, U, m.value>), dim3((unsigned)((a.n_k + 64 * V - 1) / (64 * V)), (unsigned)((a.n_q + rows - 1) / rows), (unsigned)a.c),
-                       dim3(64 * waves), rp_lds(a.nb, waves, a.mode), st, a, rows);
+    hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, U, m.value>), dim3((unsigned)((a.n_k + 64 * V - 1) / (64 * V)), (unsigned)split, (unsigned)a.c),
+                       dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a);
   });
 }
-template <typename T> void rp_bwd_run(hipStream_t st, int device, const RpArgs& a, int layout, int v, long long groups, int rows) {
+template <typename T> void rp_bwd_run(hipStream_t st, int device, const RpArgs& a, int layout, int v, long long groups, int split) {
   if (layout == PE_RELPOS_PAIR) {
-    if (a.c > 32) rp_pair_bwd<T, 1, 64>(st, device, a, groups);
-    else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, device, a, groups);
-    else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, device, a, groups);
-    else rp_pair_bwd<T, 8, 8>(st, device, a, groups);
+    if (a.c > 32) rp_pair_bwd<T, 1>(st, device, a, groups);
+    else if (a.c > 16) rp_pair_bwd<T, 2>(st, device, a, groups);
+    else if (a.c > 8) rp_pair_bwd<T, 4>(st, device, a, groups);
+    else rp_pair_bwd<T, 8>(st, device, a, groups);
   } else {
-    if (v == 8) rp_heads_bwd<T, 8>(st, device, a, rows); else if (v == 2) rp_heads_bwd<T, 2>(st, device, a, rows); else rp_heads_bwd<T, 1>(st, device, a, rows);
+    if (v == 8) rp_heads_bwd<T, 8>(st, device, a, split); else if (v == 2) rp_heads_bwd<T, 2>(st, device, a, split); else rp_heads_bwd<T, 1>(st, device, a, split);
   }
 }
 
@@ -518,11 +517,11 @@ int pe_relpos_bwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
     long long groups = 0;
     if (some) {
       const int v = pair ? 1 : Width(p->n_k, e).take(d_out, a.ld, 2).v;
-      const int rows = pair ? 0 : rp_heads_rows(*p, v);
+      const int split = pair ? 0 : rp_heads_split(*p, v);
       groups = pair ? rp_pair_groups(*p) : rp_heads_groups(*p, v);
       const double n = (double)p->n_q * p->n_k * p->c;
       op.launch("relpos bwd", pair ? "relpos_pair_bwd_kernel" : "relpos_heads_bwd_kernel", n, n * e, [&] {
-        if (p->dtype == PE_BF16) rp_bwd_run<bf16>(op.st, h->device, a, p->layout, v, groups, rows); else rp_bwd_run<float>(op.st, h->device, a, p->layout, v, groups, rows);
+        if (p->dtype == PE_BF16) rp_bwd_run<bf16>(op.st, h->device, a, p->layout, v, groups, split); else rp_bwd_run<float>(op.st, h->device, a, p->layout, v, groups, split);
       });
     }
     const int cols = a.nb * p->c;

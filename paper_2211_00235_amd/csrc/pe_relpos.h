@@ -26,8 +26,9 @@ struct RpArgs {
 };
 
 // How a bucket is found.  DENSE: the edges are consecutive integers (clipped distances), the clamped distance is the bucket.
-// LUT: the edges span at most RP_LUT distances; a byte per distance in LDS.  SEARCH: any other edges, in LDS, by bisection.  A bisection
-// is up to eight LDS reads that wait for one another: the bias gradient of 16 heads over 2048 x 2048 positions took 400 us with it.
+// LUTS: the edges span at most RP_LUT distances; a byte per distance in LDS.  SEARCH: edges in LDS, by bisection, up to eight reads that
+// wait for one another: backward of 16 heads over 2048 x 2048 positions 67 us, with the bytes 35.  The bytes take a workgroup about
+// 1 us, which pays from some ten lookups per lane on: kernels with fewer (PAIR, one row of HEADS: 4.6 us, 3.7 by bisection) search.
 enum RpMode { RP_DENSE = 0, RP_LUTS = 1, RP_SEARCH = 2 };
 constexpr int rp_lds_words(int mode) { return mode == RP_DENSE ? 1 : mode == RP_LUTS ? RP_LUT / 4 + 1 : RP_MAX_EDGES + 2; }
 
@@ -49,9 +50,12 @@ template <int MODE> struct RpBuckets {
   int n, lo, hi, other;
   // every thread of the workgroup; the caller passes a barrier before the first use
   static PE_DEV void fill(int* lds, const RpArgs& a) {
-    if constexpr (MODE == RP_LUTS) {
-      for (int i = threadIdx.x; i <= a.hi - a.lo; i += blockDim.x)
-        reinterpret_cast<uint8_t*>(lds)[i] = (uint8_t)rp_search([&](int k) { return a.edges[k]; }, a.n_edges, a.lo + i);
+    if constexpr (MODE == RP_LUTS) {      // a wave fills a bucket's bytes (a search per byte is a chain of loads: 3 us at the start of every workgroup)
+      const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+      for (int b = wave; b <= a.n_edges; b += waves) {
+        const int from = b == 0 ? 0 : a.edges[b - 1] - a.lo, to = b == a.n_edges ? a.hi - a.lo + 1 : a.edges[b] - a.lo;
+        for (int i = from + lane; i < to; i += 64) reinterpret_cast<uint8_t*>(lds)[i] = (uint8_t)b;
+      }
     }
     if constexpr (MODE == RP_SEARCH)
       for (int i = threadIdx.x; i < a.n_edges; i += blockDim.x) lds[i] = a.edges[i];
@@ -198,13 +202,13 @@ PE_DEV void lds_add(float* p, float v) { *p += v; }
 // PAIR, backward.  Lane = channel; a wave walks over positions and adds each to the LDS word [bucket][lane] of its own
 // accumulators.  Neighbouring positions of the same bucket (all that are farther than the outermost edges) are added in a register
 // first, which the whole wave decides together where it has one position at a time.  S positions share a wave where c <= 32.
-// blockIdx.y: slab of 64 channels (S = 1).  U loads are in flight per wave; lanes behind the last channel or position load a valid one,
+// blockIdx.y: slab of 64 channels (S = 1).  The loads of 64 positions are in flight per wave; lanes behind the last channel or position load a valid one,
 // since a load under a condition is waited for by itself (2 bytes per lane and 126 us at 384 x 384 x 128).
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int S, int U, int MODE>
+template <typename T, int S, int MODE>
 __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, long long per_group) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
-  constexpr int CL = 64 / S;           // lanes per position
+  constexpr int CL = 64 / S, U = 64 / S;       // lanes per position; loads per lane and 64 positions
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int sub = lane / CL, ch = blockIdx.y * 64 + lane % CL;
   int* edges = reinterpret_cast<int*>(acc + waves * a.nb * 64);
@@ -212,12 +216,13 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
   const T* g = (const T*)a.d_out + min(ch, a.c - 1);
   const long long n = (long long)a.n_q * a.n_k;
   const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
-  // a wave takes runs of 64 positions: lane l finds the place and the distance of the l-th
+  // a wave takes 64 positions, each as many behind the last as there are waves, so that every wave has its share of those whose bucket changes from one to the next: lane l
+  // finds the place and the distance of the l-th
   int cnt, pq, pk, sq, sk, rlo, rhi;
   auto locate = [&](long long p) {
-    cnt = (int)min((long long)64, p1 - p);
+    cnt = (int)min((long long)64, (p1 - p + waves - 1) / waves);
     const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
-    const int over = kk + min(lane, cnt - 1), dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
+    const int over = kk + min(lane, cnt - 1) * waves, dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
     pq = a.pos_q[q];
     pk = a.pos_k[k];
     sq = a.seg_q ? a.seg_q[q] : 0;
@@ -226,44 +231,44 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
     rlo = (int)(uint32_t)(uint64_t)row;
     rhi = (int)(uint32_t)((uint64_t)row >> 32);
   };
-  T v[U];
-  auto load = [&](int j) {
+  T next[U];
+  auto load = [&]() {
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int l = j + u * S + sub;
+      const int l = u * S + sub;
       uint32_t lo, hi;
       if constexpr (S == 1) { lo = __builtin_amdgcn_readlane(rlo, l); hi = __builtin_amdgcn_readlane(rhi, l); }
       else { lo = (uint32_t)__shfl(rlo, l, 64); hi = (uint32_t)__shfl(rhi, l, 64); }
-      v[u] = g[(long long)(((uint64_t)hi << 32) | lo)];
+      next[u] = g[(long long)(((uint64_t)hi << 32) | lo)];
     }
   };
-  long long p = p0 + wave * 64;
-  if (p < p1) { locate(p); load(0); }      // on their way while the accumulators are cleared
+  long long p = p0 + wave;
+  if (p < p1) { locate(p); load(); }       // on their way while the accumulators are cleared, and the next 64 while these are added up
   RpBuckets<MODE>::fill(edges, a);
   for (int i = threadIdx.x; i < waves * a.nb * 64; i += blockDim.x) acc[i] = 0.0f;
   __syncthreads();
   const RpBuckets<MODE> rb(edges, a);
-  for (bool first = true; p < p1; p += 64LL * waves, first = false) {
-    if (!first) { locate(p); load(0); }
-    const int b = rb.of(pq, pk, sq, sk);
+  while (p < p1) {
+    const int b = rb.of(pq, pk, sq, sk), now = cnt;
+    T v[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) v[u] = next[u];
+    p += 64LL * waves;
+    if (p < p1) { locate(p); load(); }
     int run = S == 1 ? __builtin_amdgcn_readlane(b, 0) : 0;                    // bucket of the run that is being added up
     float sum = 0.0f;
-#pragma unroll 1
-    for (int j = 0; j < cnt; j += S * U) {
-      if (j) load(j);
 #pragma unroll
-      for (int u = 0; u < U; u++) {
-        const int l = j + u * S + sub;
-        if constexpr (S == 1) {
-          const int bb = __builtin_amdgcn_readlane(b, l);
-          if (l < cnt) {
-            if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
-            sum += (float)v[u];
-          }
-        } else {
-          const int bb = __shfl(b, l, 64);
-          if (l < cnt) lds_add(mine + bb * 64, (float)v[u]);
+    for (int u = 0; u < U; u++) {
+      const int l = u * S + sub;
+      if constexpr (S == 1) {
+        const int bb = __builtin_amdgcn_readlane(b, l);
+        if (l < now) {
+          if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
+          sum += (float)v[u];
         }
+      } else {
+        const int bb = __shfl(b, l, 64);
+        if (l < now) lds_add(mine + bb * 64, (float)v[u]);
       }
     }
     if constexpr (S == 1) lds_add(mine + run * 64, sum);
@@ -282,12 +287,13 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, and adds to the LDS words
+// HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, spread over all rows so that every wave has its
+// share of those near its positions (which cost several times the others), and adds to the LDS words
 // [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).  Most lanes' positions are all farther than the outermost
 // edges, which their extremes tell: V elements are then one addition to LDS and no bucket is looked up.
 // ---------------------------------------------------------------------------------------------------------------------
 template <typename T, int V, int U, int MODE>
-__global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, int rows) {
+__global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   int* edges = reinterpret_cast<int*>(acc + waves * a.nb * 64);
@@ -297,26 +303,26 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a, i
   __syncthreads();
   const RpBuckets<MODE> rb(edges, a);
   const int h = blockIdx.z, k = (blockIdx.x * 64 + lane) * V;
-  const int q1 = min(a.n_q, (int)(blockIdx.y + 1) * rows);
+  const int step = gridDim.y * waves;                      // rows between a wave's
   if (k < a.n_k) {
     RpLane<V> at(a, k);
     const T* g = (const T*)a.d_out + (long long)h * a.n_q * a.ld + k;
     Raw<T, V> next[U];
     auto fetch = [&](int q) {
 #pragma unroll
-      for (int u = 0; u < U; u++) next[u] = raw_load<T, V>(g + (long long)min(q + u * waves, q1 - 1) * a.ld);
+      for (int u = 0; u < U; u++) next[u] = raw_load<T, V>(g + (long long)min(q + u * step, a.n_q - 1) * a.ld);
     };
-    int q = blockIdx.y * rows + wave;
-    if (q < q1) fetch(q);
-    for (; q < q1; q += U * waves) {
+    int q = blockIdx.y * waves + wave;
+    if (q < a.n_q) fetch(q);
+    for (; q < a.n_q; q += U * step) {
       Raw<T, V> v[U];
 #pragma unroll
       for (int u = 0; u < U; u++) v[u] = next[u];
-      if (q + U * waves < q1) fetch(q + U * waves);
+      if (q + U * step < a.n_q) fetch(q + U * step);
 #pragma unroll
       for (int u = 0; u < U; u++) {
-        const int qu = q + u * waves;
-        if (qu >= q1) break;
+        const int qu = q + u * step;
+        if (qu >= a.n_q) break;
         const int pq = a.pos_q[qu], sq = a.seg_q ? a.seg_q[qu] : 0;
         const int far = at.far(rb, pq, sq);
         if (far >= 0) {
