@@ -23,17 +23,12 @@ PE_DEV float ck_scale(uint32_t sb) { return sb == 255u ? __uint_as_float(0x7fc00
 PE_DEV int ck_code(float x, float inv) { return (int)rintf(x * inv); }
 
 template <int V> struct Codes;       // V consecutive codes
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 template <> struct Codes<8> {
   uint2 v;
   PE_DEV int get(int i) const { return (int)(int8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3))); }
   PE_DEV void clear() { v.x = v.y = 0; }
   PE_DEV void put(int i, int c) { (i < 4 ? v.x : v.y) |= ((uint32_t)c & 255u) << (8 * (i & 3)); }
-};
-template <> struct Codes<2> {
-  uint16_t v;
-  PE_DEV int get(int i) const { return (int)(int8_t)(v >> (8 * i)); }
-  PE_DEV void clear() { v = 0; }
-  PE_DEV void put(int i, int c) { v |= (uint16_t)(((uint32_t)c & 255u) << (8 * i)); }
 };
 template <> struct Codes<1> {
   int8_t v;
@@ -42,13 +37,29 @@ template <> struct Codes<1> {
   PE_DEV void put(int, int c) { v = (int8_t)c; }
 };
 
-// V elements of a group's 32 / V lanes -> the scale byte of the group (in all of its lanes) and this lane's codes.  Elements
-// behind the last channel have to be zero.
-template <int V> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>& codes) {
+// a lane's codes of a row (the row of codes has no gaps, so its alignment goes with c)
+template <int V, bool WHOLE> PE_DEV Codes<V> codes_load(const int8_t* row, const Slot<V, WHOLE>& s) {
+  Codes<V> c;
+  if constexpr (WHOLE || V == 1) c = *reinterpret_cast<const Codes<V>*>(row + s.at);
+  else { const u32x2_any w = *reinterpret_cast<const u32x2_any*>(row + s.at); c.v.x = w[0]; c.v.y = w[1]; }
+  return c;
+}
+template <int V, bool WHOLE> PE_DEV void codes_store(int8_t* row, const Slot<V, WHOLE>& s, const Codes<V>& c) {
+  if constexpr (WHOLE || V == 1) *reinterpret_cast<Codes<V>*>(row + s.at) = c;
+  else if (s.skip == 0) *reinterpret_cast<u32x2_any*>(row + s.at) = u32x2_any{c.v.x, c.v.y};
+  else
+#pragma unroll
+    for (int i = 1; i < V; i++)
+      if (i >= s.skip) row[s.at + i] = (int8_t)c.get(i);
+}
+
+// V elements of each of the LG lanes that share a group -> the scale byte of the group (in all of its lanes) and this lane's codes.
+// Elements that are not the lane's have to be zero.
+template <int V, int LG> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>& codes) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < V; i++) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);    // as integers NaN is above infinity above every number
-  const uint32_t sb = ck_scale_byte(lanes_umax<CK_GROUP / V>(m));
+  const uint32_t sb = ck_scale_byte(lanes_umax<LG>(m));
   const float inv = ck_inverse(sb == 255u ? 127u : sb);
   codes.clear();
 #pragma unroll
@@ -56,18 +67,20 @@ template <int V> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>& codes)
   return sb;
 }
 
-// One item = V channels of a row; a row has `per_row` items, a multiple of a group's LG = 32 / V, of which those from `n_vec` on hold no
-// channel, so item / LG numbers the groups.  A wave takes 64 U consecutive items, all of its loads in flight at once; their
-// scales are 64 U / LG consecutive bytes, stored by as many lanes together.  `flat`: no gaps and whole groups, one long row.  HBM-bound.
-template <typename T, int V, int U, bool PACK>
+// One item = V channels of a row; a row has `per_row` items, a multiple of the LG that share a group (V = 8: 4; V = 1, rows of
+// fewer than 8 channels: 8, one group per row), so item / LG numbers the groups.  A wave takes 64 U consecutive items, all of its
+// loads in flight at once; their scales are 64 U / LG consecutive bytes, stored by as many lanes together.  `flat`: no gaps and
+// whole groups, one long row.  HBM-bound.
+template <typename T, int V, bool WHOLE, int U, bool PACK>
 __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int8_t* codes, uint8_t* scales, T* y, long long rows,
                                                    int c, int per_row, int flat) {
-  constexpr int LG = CK_GROUP / V;
-  const int n_vec = c / V, lane = threadIdx.x & 63;
+  constexpr int LG = V == 8 ? 4 : 8;
+  const int lane = threadIdx.x & 63;
   const long long items = rows * per_row, first = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * U);
   const long long row0 = flat ? 0 : first / per_row;
   const uint32_t rem = flat ? 0 : (uint32_t)(first - row0 * per_row);
-  long long at[U], code_at[U];       // element offsets in x or y, and in the codes
+  long long at[U], code_at[U];       // element offsets of the row in x or y, and in the codes (flat: of the item)
+  int vec[U];
   bool in[U];
   Raw<T, V> v[U];
   Codes<V> cd[U];
@@ -75,37 +88,40 @@ __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const long long item = first + 64 * u + lane;
-    if (flat) {
+    if (WHOLE && flat) {
       in[u] = item < items;
+      vec[u] = 0;
       at[u] = code_at[u] = item * V;
     } else {
       const uint32_t off = rem + 64u * u + lane, dr = off / (uint32_t)per_row;
       const long long row = row0 + dr;
-      const int vec = (int)(off - dr * (uint32_t)per_row);
-      in[u] = item < items && vec < n_vec;
-      at[u] = row * ld + (long long)vec * V;
-      code_at[u] = row * c + (long long)vec * V;
+      vec[u] = (int)(off - dr * (uint32_t)per_row);
+      in[u] = item < items && vec[u] * V < c;
+      at[u] = row * ld;
+      code_at[u] = row * c;
     }
+    const Slot<V, WHOLE> s(vec[u], c);
     if constexpr (PACK) {
-      v[u] = in[u] ? raw_load<T, V>(x + at[u]) : raw_zero<T, V>();
+      v[u] = in[u] ? s.load(x + at[u]) : raw_zero<T, V>();
     } else if (in[u]) {
-      cd[u] = *reinterpret_cast<const Codes<V>*>(codes + code_at[u]);
+      cd[u] = codes_load(codes + code_at[u], s);
       sb[u] = scales[item / LG];
     }
   }
 #pragma unroll
   for (int u = 0; u < U; u++) {
+    const Slot<V, WHOLE> s(vec[u], c);
     if constexpr (PACK) {
       float f[V];
 #pragma unroll
-      for (int i = 0; i < V; i++) f[i] = v[u].get(i);
-      sb[u] = ck_encode<V>(f, cd[u]);
-      if (in[u]) *reinterpret_cast<Codes<V>*>(codes + code_at[u]) = cd[u];
+      for (int i = 0; i < V; i++) f[i] = s.has(i) ? v[u].get(i) : 0.0f;
+      sb[u] = ck_encode<V, LG>(f, cd[u]);
+      if (in[u]) codes_store(codes + code_at[u], s, cd[u]);
     } else if (in[u]) {
-      const float s = ck_scale(sb[u]);
+      const float scale = ck_scale(sb[u]);
 #pragma unroll
-      for (int i = 0; i < V; i++) v[u].set(i, (float)cd[u].get(i) * s);
-      raw_store<T, V>(y + at[u], v[u]);
+      for (int i = 0; i < V; i++) v[u].set(i, (float)cd[u].get(i) * scale);
+      s.store(y + at[u], v[u]);
     }
   }
   if constexpr (PACK) {
@@ -114,8 +130,8 @@ __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int
     uint32_t mine = 0;
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const uint32_t s = (uint32_t)__shfl((int)sb[u], (lane % PER) * LG, 64);
-      if (lane / PER == u) mine = s;
+      const uint32_t t = (uint32_t)__shfl((int)sb[u], (lane % PER) * LG, 64);
+      if (lane / PER == u) mine = t;
     }
     const long long group = first / LG + lane;
     if (lane < N && group < items / LG) scales[group] = (uint8_t)mine;

@@ -52,7 +52,8 @@ template <int L> PE_DEV uint32_t lanes_umax(uint32_t v) {
   return v;
 }
 
-// V consecutive elements as they lie in memory: V = 8 needs 16-byte aligned addresses, V = 2 twice the element's size
+// V consecutive elements as they lie in memory.  raw_load / raw_store: 16-byte aligned addresses for V = 8.  The _any forms need the
+// element's alignment only (global accesses of 16 bytes may start at any byte).
 template <typename T, int V> struct Raw;
 template <> struct Raw<bf16, 8> { bf16x8 v; PE_DEV float get(int i) const { return (float)v[i]; } PE_DEV void set(int i, float f) { v[i] = (bf16)f; } };
 template <> struct Raw<bf16, 2> { bf16x2 v; PE_DEV float get(int i) const { return (float)v[i]; } PE_DEV void set(int i, float f) { v[i] = (bf16)f; } };
@@ -72,17 +73,54 @@ template <typename T, int V> PE_DEV Raw<T, V> raw_zero() {
   for (int i = 0; i < V; i++) r.set(i, 0.0f);
   return r;
 }
+typedef bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+PE_DEV Raw<bf16, 8> raw_load_any(const bf16* p) { Raw<bf16, 8> r; r.v = *reinterpret_cast<const bf16x8_any*>(p); return r; }
+PE_DEV Raw<float, 8> raw_load_any(const float* p) {
+  Raw<float, 8> r;
+  r.v[0] = *reinterpret_cast<const f32x4_any*>(p);
+  r.v[1] = *reinterpret_cast<const f32x4_any*>(p + 4);
+  return r;
+}
+PE_DEV void raw_store_any(bf16* p, const Raw<bf16, 8>& r) { *reinterpret_cast<bf16x8_any*>(p) = r.v; }
+PE_DEV void raw_store_any(float* p, const Raw<float, 8>& r) {
+  *reinterpret_cast<f32x4_any*>(p) = r.v[0];
+  *reinterpret_cast<f32x4_any*>(p + 4) = r.v[1];
+}
+
+// How a lane's V of a row's c elements lie.  WHOLE: c a multiple of V, rows aligned to V elements.  Ragged (V = 8, c >= 8): any c and any
+// alignment; the last vector of a row starts at c - 8, and its first `skip` elements are the vector's before it: they are
+// loaded, count as zero, and are not stored.
+template <int V, bool WHOLE> struct Slot {
+  int at, skip;
+  bool in;
+  PE_DEV Slot(int vec, int c) {
+    if constexpr (WHOLE) { in = vec < c / V; at = vec * V; skip = 0; }
+    else { in = vec * V < c; at = min(vec * V, c - V); skip = vec * V - at; }
+  }
+  PE_DEV bool has(int i) const { return WHOLE || i >= skip; }
+  template <typename T> PE_DEV Raw<T, V> load(const T* row) const {
+    if constexpr (WHOLE) return raw_load<T, V>(row + at); else return raw_load_any(row + at);
+  }
+  template <typename T> PE_DEV void store(T* row, const Raw<T, V>& r) const {
+    if constexpr (WHOLE) raw_store<T, V>(row + at, r);
+    else if (skip == 0) raw_store_any(row + at, r);
+    else
+#pragma unroll
+      for (int i = 1; i < V; i++)
+        if (i >= skip) row[at + i] = (T)r.get(i);
+  }
+};
 
 // V consecutive fp32 numbers at an address of which only 4-byte alignment is known, in as few accesses as there are 16-byte pieces
-typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
-typedef float f32x2_u __attribute__((ext_vector_type(2), aligned(4)));
 template <int V> PE_DEV void load_f32(const float* p, float (&v)[V]) {
   if constexpr (V == 8) {
-    const f32x4_u a = *reinterpret_cast<const f32x4_u*>(p), b = *reinterpret_cast<const f32x4_u*>(p + 4);
+    const f32x4_any a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
 #pragma unroll
     for (int i = 0; i < 4; i++) { v[i] = a[i]; v[4 + i] = b[i]; }
   } else if constexpr (V == 2) {
-    const f32x2_u a = *reinterpret_cast<const f32x2_u*>(p);
+    const f32x2_any a = *reinterpret_cast<const f32x2_any*>(p);
     v[0] = a[0]; v[1] = a[1];
   } else {
     v[0] = *p;

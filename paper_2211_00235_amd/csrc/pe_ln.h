@@ -5,8 +5,9 @@
 //   d_gain = sum over rows of dy z,  d_offset = sum over rows of dy
 //
 // HBM-bound: 8 vector operations per element forward, 15 backward, against 4 to 8 bytes.  A row lies in the registers of L
-// lanes (NV vectors of V elements each), so that it is read once: L = 4..64 lanes, several rows per wave, up to 2048 channels,
-// whole workgroups above.  Statistics and sums are fp32; a result is rounded once, to the storage type.  A lane keeps its columns'
+// lanes (NV vectors of V elements each), so that it is read once: L = 4..64 lanes, several rows per wave, up to 1024 channels,
+// whole workgroups above.  Channel counts and alignments without 16-byte accesses take the same kernels with WHOLE = false; rows of fewer
+// than 8 channels have a lane per channel.  Statistics and sums are fp32; a result is rounded once, to the storage type.  A lane keeps its columns'
 // d_gain and d_offset in registers over all of its rows; workgroups write one fp32 partial each, and columns_sum_kernel adds
 // them in a fixed order.
 #pragma once
@@ -63,23 +64,22 @@ template <int L> struct LnShape {
   static constexpr int ROWS = THREADS / L;
 };
 
-template <typename T, int V, int L, int NV>
+template <typename T, int V, bool WHOLE, int L, int NV>
 __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const LnArgs a) {
-  constexpr int ROWS = LnShape<L>::ROWS, LG = CK_GROUP / V;
+  constexpr int ROWS = LnShape<L>::ROWS, LG = V == 8 ? 4 : 8;
   __shared__ float red[4][16];
   const int li = threadIdx.x % L;                        // this lane's place in its row
-  const int c = a.c, n_vec = c / V;
+  const int c = a.c, groups = (c + CK_GROUP - 1) / CK_GROUP;
   const float inv_c = 1.0f / (float)c;
-  bool in[NV];
-#pragma unroll
-  for (int n = 0; n < NV; n++) in[n] = n * L + li < n_vec;
+  auto slot_of = [&](int n) { return Slot<V, WHOLE>(n * L + li, c); };
   float gain[NV][V], offs[NV][V];
 #pragma unroll
   for (int n = 0; n < NV; n++) {
 #pragma unroll
     for (int i = 0; i < V; i++) { gain[n][i] = 1.0f; offs[n][i] = 0.0f; }
-    if (in[n] && a.gain) load_f32<V>(a.gain + (n * L + li) * V, gain[n]);
-    if (in[n] && a.offset) load_f32<V>(a.offset + (n * L + li) * V, offs[n]);
+    const auto sl = slot_of(n);
+    if (sl.in && a.gain) load_f32<V>(a.gain + sl.at, gain[n]);
+    if (sl.in && a.offset) load_f32<V>(a.offset + sl.at, offs[n]);
   }
   const T* x = (const T*)a.x;
   const T* add = (const T*)a.add;
@@ -89,8 +89,10 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
   Raw<T, V> next[NV];
   auto fetch = [&](long long r) {
 #pragma unroll
-    for (int n = 0; n < NV; n++)
-      next[n] = in[n] && r < a.rows ? raw_load<T, V>(x + r * a.ld_x + (n * L + li) * V) : raw_zero<T, V>();
+    for (int n = 0; n < NV; n++) {
+      const auto sl = slot_of(n);
+      next[n] = sl.in && r < a.rows ? sl.load(x + r * a.ld_x) : raw_zero<T, V>();
+    }
   };
   fetch(row);
   int slot = 0;
@@ -100,22 +102,25 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
     for (int n = 0; n < NV; n++) v[n] = next[n];
     if (add) {
 #pragma unroll
-      for (int n = 0; n < NV; n++)
-        if (in[n]) ad[n] = raw_load<T, V>(add + row * a.ld_add + (n * L + li) * V);
+      for (int n = 0; n < NV; n++) {
+        const auto sl = slot_of(n);
+        if (sl.in) ad[n] = sl.load(add + row * a.ld_add);
+      }
     }
     fetch(row + step);
     float s = 0.0f;
 #pragma unroll
     for (int n = 0; n < NV; n++)
 #pragma unroll
-      for (int i = 0; i < V; i++) s += v[n].get(i);
+      for (int i = 0; i < V; i++) s += slot_of(n).has(i) ? v[n].get(i) : 0.0f;
     const float mean = row_sum<L>(s, red[slot]) * inv_c;
     float q = 0.0f;
 #pragma unroll
     for (int n = 0; n < NV; n++)
 #pragma unroll
       for (int i = 0; i < V; i++) {
-        const float t = in[n] ? v[n].get(i) - mean : 0.0f;
+        const auto sl = slot_of(n);
+        const float t = sl.in && sl.has(i) ? v[n].get(i) - mean : 0.0f;
         q += t * t;
       }
     const float rstd = rsqrtf(row_sum<L>(q, red[slot + 1]) * inv_c + a.eps);
@@ -129,41 +134,39 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_fwd_kernel(const Ln
         if (add) f += ad[n].get(i);
         o.set(i, f);
       }
-      if (in[n]) raw_store<T, V>(y + row * a.ld_out + (n * L + li) * V, o);
-      if constexpr (L >= LG) {
-        if (a.k_codes) {
-          float f[V];
+      const auto sl = slot_of(n);
+      if (sl.in) sl.store(y + row * a.ld_out, o);
+      if (a.k_codes) {
+        float f[V];
 #pragma unroll
-          for (int i = 0; i < V; i++) f[i] = v[n].get(i);
-          Codes<V> cd;
-          const uint32_t sb = ck_encode<V>(f, cd);
-          if (in[n]) {
-            const int vec = n * L + li;
-            *reinterpret_cast<Codes<V>*>(a.k_codes + row * c + vec * V) = cd;
-            if (vec % LG == 0) a.k_scales[row * ((c + CK_GROUP - 1) / CK_GROUP) + vec / LG] = (uint8_t)sb;
-          }
+        for (int i = 0; i < V; i++) f[i] = sl.has(i) ? v[n].get(i) : 0.0f;
+        Codes<V> cd;
+        const uint32_t sb = ck_encode<V, LG>(f, cd);
+        if (sl.in) {
+          const int vec = n * L + li;
+          codes_store(a.k_codes + row * c, sl, cd);
+          if (vec % LG == 0) a.k_scales[row * groups + vec / LG] = (uint8_t)sb;
         }
       }
     }
   }
 }
 
-template <typename T, int V, int L, int NV, bool KEPT>
+template <typename T, int V, bool WHOLE, int L, int NV, bool KEPT>
 __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const LnArgs a) {
-  constexpr int ROWS = LnShape<L>::ROWS, LG = CK_GROUP / V, W = LnShape<L>::THREADS / 64;
+  constexpr int ROWS = LnShape<L>::ROWS, LG = V == 8 ? 4 : 8, W = LnShape<L>::THREADS / 64;
   __shared__ float red[4][16];
   const int li = threadIdx.x % L;
-  const int c = a.c, n_vec = c / V, groups = (c + CK_GROUP - 1) / CK_GROUP;
+  const int c = a.c, groups = (c + CK_GROUP - 1) / CK_GROUP;
   const float inv_c = 1.0f / (float)c;
-  bool in[NV];
-#pragma unroll
-  for (int n = 0; n < NV; n++) in[n] = n * L + li < n_vec;
+  auto slot_of = [&](int n) { return Slot<V, WHOLE>(n * L + li, c); };
   float gain[NV][V], dg[NV][V], db[NV][V];
 #pragma unroll
   for (int n = 0; n < NV; n++) {
 #pragma unroll
     for (int i = 0; i < V; i++) { gain[n][i] = 1.0f; dg[n][i] = db[n][i] = 0.0f; }
-    if (in[n] && a.gain) load_f32<V>(a.gain + (n * L + li) * V, gain[n]);
+    const auto sl = slot_of(n);
+    if (sl.in && a.gain) load_f32<V>(a.gain + sl.at, gain[n]);
   }
   const T* x = (const T*)a.x;
   const T* dy = (const T*)a.dy;
@@ -180,18 +183,18 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
     nst = live ? *reinterpret_cast<const f32x2*>(a.stats_in + 2 * r) : f32x2{0.0f, 0.0f};
 #pragma unroll
     for (int n = 0; n < NV; n++) {
-      const int vec = n * L + li;
-      const bool on = in[n] && live;
-      ny[n] = on ? raw_load<T, V>(dy + r * a.ld_dy + vec * V) : raw_zero<T, V>();
+      const auto sl = slot_of(n);
+      const bool on = sl.in && live;
+      ny[n] = on ? sl.load(dy + r * a.ld_dy) : raw_zero<T, V>();
       if constexpr (KEPT) {
         nc[n].clear();
         nsb[n] = 0;
         if (on) {
-          nc[n] = *reinterpret_cast<const Codes<V>*>(a.codes + r * c + vec * V);
-          nsb[n] = a.scales[r * groups + vec / LG];
+          nc[n] = codes_load(a.codes + r * c, sl);
+          nsb[n] = a.scales[r * groups + (n * L + li) / LG];
         }
       } else {
-        nx[n] = on ? raw_load<T, V>(x + r * a.ld_x + vec * V) : raw_zero<T, V>();
+        nx[n] = on ? sl.load(x + r * a.ld_x) : raw_zero<T, V>();
       }
     }
   };
@@ -211,8 +214,10 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
     }
     if (add && dx) {
 #pragma unroll
-      for (int n = 0; n < NV; n++)
-        if (in[n]) ad[n] = raw_load<T, V>(add + row * a.ld_add + (n * L + li) * V);
+      for (int n = 0; n < NV; n++) {
+        const auto sl = slot_of(n);
+        if (sl.in) ad[n] = sl.load(add + row * a.ld_add);
+      }
     }
     if constexpr (AHEAD) fetch(row + step);
     auto z_of = [&](int n, int i) {
@@ -225,7 +230,8 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
     for (int n = 0; n < NV; n++)
 #pragma unroll
       for (int i = 0; i < V; i++) {
-        const float d = y[n].get(i), z = in[n] ? z_of(n, i) : 0.0f, u = d * gain[n][i];
+        const auto sl = slot_of(n);
+        const float d = sl.has(i) ? y[n].get(i) : 0.0f, z = sl.in && sl.has(i) ? z_of(n, i) : 0.0f, u = d * gain[n][i];
         dg[n][i] += d * z;
         db[n][i] += d;
         s1 += u;
@@ -243,7 +249,8 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
           if (add) f += ad[n].get(i);
           o.set(i, f);
         }
-        if (in[n]) raw_store<T, V>(dx + row * a.ld_out + (n * L + li) * V, o);
+        const auto sl = slot_of(n);
+        if (sl.in) sl.store(dx + row * a.ld_out, o);
       }
     }
   }
@@ -261,24 +268,27 @@ __global__ __launch_bounds__(LnShape<L>::THREADS) void ln_op_bwd_kernel(const Ln
       }
       __syncthreads();
       for (int k = threadIdx.x; k < 2 * L * V; k += LnShape<L>::THREADS) {
-        const int t = k / (L * V), e = k % (L * V), ch = n * L * V + e;
+        const int t = k / (L * V), e = k % (L * V);
+        const Slot<V, WHOLE> sl(n * L + e / V, c);
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < W; w++) s += (&cols[t][w][0][0])[e];
-        if (ch < c) part[t * c + ch] = s;
+        if (sl.in && sl.has(e % V)) part[t * c + sl.at + e % V] = s;
       }
       __syncthreads();
     }
   } else {                     // every column is one lane's
 #pragma unroll
-    for (int n = 0; n < NV; n++)
-      if (in[n])
+    for (int n = 0; n < NV; n++) {
+      const auto sl = slot_of(n);
+      if (sl.in)
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-          const int ch = (n * L + li) * V + i;
-          part[ch] = dg[n][i];
-          part[c + ch] = db[n][i];
-        }
+        for (int i = 0; i < V; i++)
+          if (sl.has(i)) {
+            part[sl.at + i] = dg[n][i];
+            part[c + sl.at + i] = db[n][i];
+          }
+    }
   }
 }
 

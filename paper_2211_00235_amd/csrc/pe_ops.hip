@@ -65,19 +65,25 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p) % a == 0; }
 // bytes from the first to the last element of [rows][c] with row stride ld
 size_t span(long long rows, long long c, long long ld, size_t e) { return rows > 0 && c > 0 ? ((size_t)(rows - 1) * ld + c) * e : 0; }
 
-// Elements per access: 8 (16-byte accesses), 2 or 1, whichever the channel count, the row strides and the addresses allow.
-struct Width {
-  int v;
+// WHOLE: rows of whole 8-element vectors, all of them aligned for 16-byte accesses
+struct Whole {
+  bool ok;
   size_t e;
-  Width(int c, size_t elem_bytes) : v(c % 8 == 0 ? 8 : c % 2 == 0 ? 2 : 1), e(elem_bytes) {}
-  Width& take(const void* p, long long ld, long long rows) {
-    if (!p) return *this;
-    if (rows <= 1) ld = 0;
-    if (v == 8 && (!aligned(p, 16) || (ld * (long long)e) % 16)) v = 2;
-    if (v == 2 && (!aligned(p, 2 * e) || ld % 2)) v = 1;
+  Whole(long long c, size_t elem_bytes) : ok(c % 8 == 0), e(elem_bytes) {}
+  Whole& take(const void* p, long long ld, long long rows) {
+    if (p && (!aligned(p, 16) || (rows > 1 && (ld * (long long)e) % 16))) ok = false;
     return *this;
   }
 };
+// calls `f` with V and WHOLE as template arguments: rows of fewer than 8 elements an element at a time
+template <typename F> void width_dispatch(long long c, bool whole, F&& f) {
+  if (c < 8) f(std::integral_constant<int, 1>{}, std::true_type{});
+  else if (whole) f(std::integral_constant<int, 8>{}, std::true_type{});
+  else f(std::integral_constant<int, 8>{}, std::false_type{});
+}
+template <typename F> void type_dispatch(int dtype, F&& f) {
+  if (dtype == PE_BF16) f(bf16{}); else f(float{});
+}
 
 constexpr int LN_MAX_C = 16384;
 constexpr long long MAX_ROWS = 1LL << 40;
@@ -89,24 +95,17 @@ constexpr int CK_MAX_C = 1 << 20;
 long long ck_groups(int c) { return (c + CK_GROUP - 1) / CK_GROUP; }
 size_t ck_bytes(long long rows, int c) { return up256((size_t)rows * c) + (size_t)rows * ck_groups(c); }
 
-template <typename T, int V, bool PACK>
-void ck_launch(hipStream_t st, const void* x, long long ld, void* ckpt, void* y, long long rows, int c) {
-  constexpr int U = V == 8 ? 4 : 8;
-  const int per_row = (int)ck_groups(c) * (CK_GROUP / V);
-  const long long items = rows * per_row, blocks = (items + 256 * U - 1) / (256 * U);
-  hipLaunchKernelGGL((ckpt_kernel<T, V, U, PACK>), dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
-                     (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row, (int)(c % CK_GROUP == 0 && (ld == c || rows == 1)));
-}
-template <bool PACK> void ck_run(hipStream_t st, int dtype, int v, const void* x, long long ld, void* ckpt, void* y, long long rows, int c) {
-  if (dtype == PE_BF16) {
-    if (v == 8) ck_launch<bf16, 8, PACK>(st, x, ld, ckpt, y, rows, c);
-    else if (v == 2) ck_launch<bf16, 2, PACK>(st, x, ld, ckpt, y, rows, c);
-    else ck_launch<bf16, 1, PACK>(st, x, ld, ckpt, y, rows, c);
-  } else {
-    if (v == 8) ck_launch<float, 8, PACK>(st, x, ld, ckpt, y, rows, c);
-    else if (v == 2) ck_launch<float, 2, PACK>(st, x, ld, ckpt, y, rows, c);
-    else ck_launch<float, 1, PACK>(st, x, ld, ckpt, y, rows, c);
-  }
+template <bool PACK> void ck_run(hipStream_t st, int dtype, bool whole, const void* x, long long ld, void* ckpt, void* y, long long rows, int c) {
+  type_dispatch(dtype, [&](auto t) {
+    using T = decltype(t);
+    width_dispatch(c, whole, [&](auto v, auto w) {
+      constexpr int V = v.value, U = 4;
+      const int per_row = V == 8 ? (int)ck_groups(c) * 4 : 8;
+      const long long items = rows * per_row, blocks = (items + 256 * U - 1) / (256 * U);
+      hipLaunchKernelGGL((ckpt_kernel<T, V, w.value, U, PACK>), dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
+                         (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row, (int)(c % CK_GROUP == 0 && (ld == c || rows == 1)));
+    });
+  });
 }
 
 int ck_call(pe_handle* h, long long rows, int c, int dtype, const void* t, long long ld, const void* ckpt, bool pack, void* stream) {
@@ -122,11 +121,11 @@ int ck_call(pe_handle* h, long long rows, int c, int dtype, const void* t, long 
   const Region rg[] = {{t, span(rows, c, ld, e), !pack}, {ckpt, ck_bytes(rows, c), pack}};
   if (any_alias(rg, 2)) return op.refuse(PE_ERR_ALIAS, "checkpoint: tensor and checkpoint overlap");
   if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "checkpoint: the handle belongs to another device than the current one");
-  const int v = Width(c, e).take(t, ld, rows).v;
+  const bool whole = Whole(c, e).take(t, ld, rows).ok;
   const double n = (double)rows * c, bytes = n * e + ck_bytes(rows, c);
   op.launch(pack ? "ckpt pack" : "ckpt unpack", "ckpt_kernel", 2 * n, bytes, [&] {
-    if (pack) ck_run<true>(op.st, dtype, v, t, ld, const_cast<void*>(ckpt), nullptr, rows, c);
-    else ck_run<false>(op.st, dtype, v, nullptr, ld, const_cast<void*>(ckpt), const_cast<void*>(t), rows, c);
+    if (pack) ck_run<true>(op.st, dtype, whole, t, ld, const_cast<void*>(ckpt), nullptr, rows, c);
+    else ck_run<false>(op.st, dtype, whole, nullptr, ld, const_cast<void*>(ckpt), const_cast<void*>(t), rows, c);
   });
   return op.err;
 }
@@ -134,61 +133,54 @@ int ck_call(pe_handle* h, long long rows, int c, int dtype, const void* t, long 
 // ---------------------------------------------------------------------------------------------------------------------
 // Layer norm
 // ---------------------------------------------------------------------------------------------------------------------
-// Lanes and vectors per lane of a row of c channels in accesses of v elements
+// Lanes and vectors per lane of a row of c channels
 struct LnPlan { int l, nv; int rows() const { return l > 256 ? 1 : 256 / l; } };
-LnPlan ln_plan(int c, int v) {
-  const int n = c / v;
-  if (v == 8) {
-    if (n <= 4) return {4, 1};
-    if (n <= 8) return {8, 1};
-    if (n <= 16) return {16, 1};
-    if (n <= 32) return {32, 1};
-    if (n <= 64) return {64, 1};
-    if (n <= 128) return {64, 2};
-    if (n <= 512) return {256, 2};
-    if (n <= 1024) return {512, 2};
-    return {1024, 2};
-  }
+LnPlan ln_plan(int c) {
+  if (c < 8) return {8, 1};
+  const int n = (c + 7) / 8;
+  if (n <= 4) return {4, 1};
+  if (n <= 8) return {8, 1};
+  if (n <= 16) return {16, 1};
+  if (n <= 32) return {32, 1};
   if (n <= 64) return {64, 1};
-  if (n <= 256) return {64, 4};
-  if (n <= 1024) return {256, 4};
-  if (n <= 4096) return {1024, 4};
-  return v == 2 ? LnPlan{1024, 8} : LnPlan{1024, 16};
+  if (n <= 128) return {64, 2};
+  if (n <= 512) return {256, 2};
+  if (n <= 1024) return {512, 2};
+  return {1024, 2};
 }
 // Most workgroups of a launch: they walk over the rows.  Backward, each writes 8 c bytes of partial sums: as many as the chip holds at once,
 // four per CU of rows within waves, two or one of rows of whole workgroups (4096 x 8192 with 512 of them 60 us and 11 for the sums,
 // with 256 49 and 7).
 constexpr int LN_FWD_WG = 2048, LN_BWD_WG = 1024;
-long long ln_bwd_groups(long long rows, int c, int v) {
-  const LnPlan p = ln_plan(c, v);
+long long ln_bwd_groups(long long rows, int c) {
+  const LnPlan p = ln_plan(c);
   return std::min<long long>((rows + p.rows() - 1) / p.rows(), p.l <= 64 ? LN_BWD_WG : p.l == 256 ? 512 : 256);
 }
 
-template <typename T, int V, int L, int NV> void ln_fwd_launch(hipStream_t st, const LnArgs& a) {
-  const long long wg = (a.rows + LnShape<L>::ROWS - 1) / LnShape<L>::ROWS;
-  hipLaunchKernelGGL((ln_op_fwd_kernel<T, V, L, NV>), dim3((unsigned)std::min<long long>(wg, LN_FWD_WG)), dim3(LnShape<L>::THREADS), 0, st, a);
-}
-template <typename T, int V, int L, int NV> void ln_bwd_launch(hipStream_t st, const LnArgs& a, unsigned wg) {
-  if (a.codes) hipLaunchKernelGGL((ln_op_bwd_kernel<T, V, L, NV, true>), dim3(wg), dim3(LnShape<L>::THREADS), 0, st, a);
-  else hipLaunchKernelGGL((ln_op_bwd_kernel<T, V, L, NV, false>), dim3(wg), dim3(LnShape<L>::THREADS), 0, st, a);
-}
 // calls `f` with the plan's template arguments
-template <int V, typename F> void ln_dispatch(const LnPlan& p, F&& f) {
+template <typename F> void ln_dispatch(const LnPlan& p, F&& f) {
 #define PE_LN_CASE(L, NV) if (p.l == L && p.nv == NV) return f(std::integral_constant<int, L>{}, std::integral_constant<int, NV>{})
-  if constexpr (V == 8) {
-    PE_LN_CASE(4, 1); PE_LN_CASE(8, 1); PE_LN_CASE(16, 1); PE_LN_CASE(32, 1); PE_LN_CASE(64, 1);
-    PE_LN_CASE(64, 2); PE_LN_CASE(256, 2); PE_LN_CASE(512, 2); PE_LN_CASE(1024, 2);
-  } else {
-    PE_LN_CASE(64, 1); PE_LN_CASE(64, 4); PE_LN_CASE(256, 4); PE_LN_CASE(1024, 4);
-    if constexpr (V == 2) { PE_LN_CASE(1024, 8); } else { PE_LN_CASE(1024, 16); }
-  }
+  PE_LN_CASE(4, 1); PE_LN_CASE(8, 1); PE_LN_CASE(16, 1); PE_LN_CASE(32, 1); PE_LN_CASE(64, 1);
+  PE_LN_CASE(64, 2); PE_LN_CASE(256, 2); PE_LN_CASE(512, 2); PE_LN_CASE(1024, 2);
 #undef PE_LN_CASE
 }
-template <typename T, int V> void ln_fwd_run(hipStream_t st, const LnArgs& a) {
-  ln_dispatch<V>(ln_plan(a.c, V), [&](auto l, auto nv) { ln_fwd_launch<T, V, l.value, nv.value>(st, a); });
+template <typename T, int V, bool WHOLE> void ln_fwd_run(hipStream_t st, const LnArgs& a) {
+  auto launch = [&](auto l, auto nv) {
+    constexpr int L = l.value;
+    const long long wg = (a.rows + LnShape<L>::ROWS - 1) / LnShape<L>::ROWS;
+    hipLaunchKernelGGL((ln_op_fwd_kernel<T, V, WHOLE, L, nv.value>), dim3((unsigned)std::min<long long>(wg, LN_FWD_WG)), dim3(LnShape<L>::THREADS), 0, st, a);
+  };
+  if constexpr (V == 1) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+  else ln_dispatch(ln_plan(a.c), launch);
 }
-template <typename T, int V> void ln_bwd_run(hipStream_t st, const LnArgs& a, unsigned wg) {
-  ln_dispatch<V>(ln_plan(a.c, V), [&](auto l, auto nv) { ln_bwd_launch<T, V, l.value, nv.value>(st, a, wg); });
+template <typename T, int V, bool WHOLE> void ln_bwd_run(hipStream_t st, const LnArgs& a, unsigned wg) {
+  auto launch = [&](auto l, auto nv) {
+    constexpr int L = l.value;
+    if (a.codes) hipLaunchKernelGGL((ln_op_bwd_kernel<T, V, WHOLE, L, nv.value, true>), dim3(wg), dim3(LnShape<L>::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((ln_op_bwd_kernel<T, V, WHOLE, L, nv.value, false>), dim3(wg), dim3(LnShape<L>::THREADS), 0, st, a);
+  };
+  if constexpr (V == 1) launch(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+  else ln_dispatch(ln_plan(a.c), launch);
 }
 void columns_sum(OpCall& op, const char* label, const float* part, long long n_part, int cols, float* o0, float* o1, int split, bool acc) {
   op.launch(label, "columns_sum_kernel", (double)n_part * cols, 4.0 * ((double)n_part * cols + cols), [&] {
@@ -223,17 +215,17 @@ long long rp_pair_groups(const pe_relpos& p) {
   const long long n = (long long)p.n_q * p.n_k;
   return std::max<long long>(1, std::min<long long>(128, (n + 511) / 512));
 }
-// HEADS: workgroups that share the rows q of a head and 64 v positions k, so that about 512 share the work, with a row per wave at least
-int rp_heads_split(const pe_relpos& p, int v) {
-  const long long tiles = (p.n_k + 64LL * v - 1) / (64LL * v) * p.c;
-  return (int)std::min<long long>((p.n_q + 7) / 8, std::max<long long>(1, (512 + tiles - 1) / tiles));
+// HEADS: 64 vectors of 8 positions k (fewer than 8: of one) per workgroup; so many workgroups share the rows q of those and of a head
+// that there are about 512, with a row per wave at least
+long long rp_heads_tiles(const pe_relpos& p) { return ((p.n_k < 8 ? p.n_k : (p.n_k + 7) / 8) + 63LL) / 64; }
+int rp_heads_split(const pe_relpos& p) {
+  const long long all = rp_heads_tiles(p) * p.c;
+  return (int)std::min<long long>((p.n_q + 7) / 8, std::max<long long>(1, (512 + all - 1) / all));
 }
-long long rp_heads_groups(const pe_relpos& p, int v) { return (long long)((p.n_k + 64 * v - 1) / (64 * v)) * rp_heads_split(p, v); }
+long long rp_heads_groups(const pe_relpos& p) { return rp_heads_tiles(p) * rp_heads_split(p); }
 size_t rp_workspace(const pe_relpos& p) {
   if (p.n_q == 0 || p.n_k == 0) return 256;
-  const long long g = p.layout == PE_RELPOS_PAIR ? rp_pair_groups(p)
-                                                 : std::max(rp_heads_groups(p, 8), std::max(rp_heads_groups(p, 2), rp_heads_groups(p, 1)));
-  return up256((size_t)g * rp_buckets(p) * p.c * 4);
+  return up256((size_t)(p.layout == PE_RELPOS_PAIR ? rp_pair_groups(p) : rp_heads_groups(p)) * rp_buckets(p) * p.c * 4);
 }
 
 // The checks that forward and backward share; on PE_OK `a` is filled but for the tensors of the direction
@@ -276,6 +268,7 @@ template <typename F> void rp_dispatch(int mode, bool few, F&& f) {
 template <typename F> void rp_dispatch_few(int mode, F&& f) {
   if (mode == RP_DENSE) f(std::integral_constant<int, RP_DENSE>{}); else f(std::integral_constant<int, RP_SEARCH>{});
 }
+// PAIR, channels per access: 8 (16 bytes) or 1
 template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
   constexpr int U = V == 8 ? 4 : 8;
   const int vecs = a.c / V;
@@ -284,7 +277,7 @@ template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
   const unsigned gx = (unsigned)((a.n_k + tile - 1) / tile), gy = (unsigned)std::min(a.n_q, 65535), gz = (unsigned)((a.n_q + 65534) / 65535);
   rp_dispatch_few(a.mode, [&](auto m) { hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U, m.value>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile, magic); });
 }
-template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) {
+template <typename T, int V, bool WHOLE> void rp_heads_fwd(hipStream_t st, const RpArgs& a) {
   // heads per workgroup: what 32 KB of LDS hold, and few enough that the chip is filled
   const long long tiles = (a.n_k + 256LL * V - 1) / (256LL * V);
   int heads = std::max(1, std::min(a.c, 32 * 1024 / (a.nb * 4)));
@@ -294,16 +287,9 @@ template <typename T, int V> void rp_heads_fwd(hipStream_t st, const RpArgs& a) 
   const long long all = tiles * gz;
   const int rows = (int)std::max<long long>((a.n_q + 65534) / 65535, std::min<long long>(16, a.n_q * all / 512));
   rp_dispatch(a.mode, rows * V < 10, [&](auto m) {
-    hipLaunchKernelGGL((relpos_heads_fwd_kernel<T, V, m.value>), dim3((unsigned)tiles, (unsigned)((a.n_q + rows - 1) / rows), gz), dim3(256),
+    hipLaunchKernelGGL((relpos_heads_fwd_kernel<T, V, WHOLE, m.value>), dim3((unsigned)tiles, (unsigned)((a.n_q + rows - 1) / rows), gz), dim3(256),
                        (size_t)heads * a.nb * 4, st, a, heads, rows);
   });
-}
-template <typename T> void rp_fwd_run(hipStream_t st, const RpArgs& a, int layout, int v) {
-  if (layout == PE_RELPOS_PAIR) {
-    if (v == 8) rp_pair_fwd<T, 8>(st, a); else if (v == 2) rp_pair_fwd<T, 2>(st, a); else rp_pair_fwd<T, 1>(st, a);
-  } else {
-    if (v == 8) rp_heads_fwd<T, 8>(st, a); else if (v == 2) rp_heads_fwd<T, 2>(st, a); else rp_heads_fwd<T, 1>(st, a);
-  }
 }
 // Dynamic LDS above 64 KB has to be allowed once per kernel and device
 template <typename K> void allow_lds(K kern, int device, std::atomic<unsigned long long>& done) {
@@ -321,35 +307,31 @@ template <typename T, int S> void rp_pair_bwd(hipStream_t st, int device, const 
                        rp_lds(a.nb, waves, m.value), st, a, (n + groups - 1) / groups);
   });
 }
-template <typename T, int V> void rp_heads_bwd(hipStream_t st, int device, const RpArgs& a, int split) {
+template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int device, const RpArgs& a, int split) {
   constexpr int U = V == 8 ? 4 : 8;
   const int waves = rp_waves(a.nb);
   rp_dispatch(a.mode, (long long)V * a.n_q < 10LL * split * waves, [&](auto m) {
     static std::atomic<unsigned long long> done{0};
-    allow_lds(&relpos_heads_bwd_kernel<T, V, U, m.value>, device, done);
-    hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, U, m.value>), dim3((unsigned)((a.n_k + 64 * V - 1) / (64 * V)), (unsigned)split, (unsigned)a.c),
+    allow_lds(&relpos_heads_bwd_kernel<T, V, WHOLE, U, m.value>, device, done);
+    hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, WHOLE, U, m.value>), dim3((unsigned)(((a.n_k + V - 1) / V + 63) / 64), (unsigned)split, (unsigned)a.c),
                        dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a);
   });
 }
-template <typename T> void rp_bwd_run(hipStream_t st, int device, const RpArgs& a, int layout, int v, long long groups, int split) {
-  if (layout == PE_RELPOS_PAIR) {
-    if (a.c > 32) rp_pair_bwd<T, 1>(st, device, a, groups);
-    else if (a.c > 16) rp_pair_bwd<T, 2>(st, device, a, groups);
-    else if (a.c > 8) rp_pair_bwd<T, 4>(st, device, a, groups);
-    else rp_pair_bwd<T, 8>(st, device, a, groups);
-  } else {
-    if (v == 8) rp_heads_bwd<T, 8>(st, device, a, split); else if (v == 2) rp_heads_bwd<T, 2>(st, device, a, split); else rp_heads_bwd<T, 1>(st, device, a, split);
-  }
+template <typename T> void rp_pair_bwd_run(hipStream_t st, int device, const RpArgs& a, long long groups) {
+  if (a.c > 32) rp_pair_bwd<T, 1>(st, device, a, groups);
+  else if (a.c > 16) rp_pair_bwd<T, 2>(st, device, a, groups);
+  else if (a.c > 8) rp_pair_bwd<T, 4>(st, device, a, groups);
+  else rp_pair_bwd<T, 8>(st, device, a, groups);
 }
 
 }  // namespace
 
 hipError_t ckpt_pack_launch(hipStream_t st, int dtype, const void* x, void* ckpt, long long rows, int c) {
-  ck_run<true>(st, dtype, 8, x, c, ckpt, nullptr, rows, c);
+  ck_run<true>(st, dtype, true, x, c, ckpt, nullptr, rows, c);
   return hipGetLastError();
 }
 hipError_t ckpt_unpack_launch(hipStream_t st, int dtype, const void* ckpt, void* y, long long rows, int c) {
-  ck_run<false>(st, dtype, 8, nullptr, c, const_cast<void*>(ckpt), y, rows, c);
+  ck_run<false>(st, dtype, true, nullptr, c, const_cast<void*>(ckpt), y, rows, c);
   return hipGetLastError();
 }
 
@@ -370,10 +352,7 @@ int pe_ckpt_unpack(pe_handle* h, long long rows, int c, int dtype, const void* c
 
 size_t pe_layernorm_workspace_bytes(long long rows, int c) {
   if (rows < 0 || rows > MAX_ROWS || c < 1 || c > LN_MAX_C) return 0;
-  long long g = 1;
-  for (int v : {8, 2, 1})
-    if (c % v == 0) g = std::max(g, ln_bwd_groups(rows, c, v));
-  return up256((size_t)g * 2 * c * 4);
+  return up256((size_t)std::max(1LL, ln_bwd_groups(rows, c)) * 2 * c * 4);
 }
 
 int pe_layernorm_fwd(pe_handle* h, long long rows, int c, int dtype, const void* x, long long ld_x, const void* add, long long ld_add,
@@ -400,11 +379,10 @@ int pe_layernorm_fwd(pe_handle* h, long long rows, int c, int dtype, const void*
     a.x = x; a.ld_x = ld_x; a.add = add; a.ld_add = ld_add; a.out = y; a.ld_out = ld_y; a.gain = gain; a.offset = offset; a.stats = stats;
     a.rows = rows; a.c = c; a.eps = eps;
     if (ckpt) { a.k_codes = (int8_t*)ckpt; a.k_scales = (uint8_t*)ckpt + up256((size_t)rows * c); }
-    const int v = Width(c, e).take(x, ld_x, rows).take(add, ld_add, rows).take(y, ld_y, rows).v;
+    const bool whole = Whole(c, e).take(x, ld_x, rows).take(add, ld_add, rows).take(y, ld_y, rows).ok;
     const double n = (double)rows * c;
     op.launch("layernorm fwd", "ln_op_fwd_kernel", 9 * n, n * e * (add ? 3 : 2) + (ckpt ? (double)ck_bytes(rows, c) : 0.0), [&] {
-      if (dtype == PE_BF16) { if (v == 8) ln_fwd_run<bf16, 8>(op.st, a); else if (v == 2) ln_fwd_run<bf16, 2>(op.st, a); else ln_fwd_run<bf16, 1>(op.st, a); }
-      else { if (v == 8) ln_fwd_run<float, 8>(op.st, a); else if (v == 2) ln_fwd_run<float, 2>(op.st, a); else ln_fwd_run<float, 1>(op.st, a); }
+      type_dispatch(dtype, [&](auto t) { width_dispatch(c, whole, [&](auto v, auto w) { ln_fwd_run<decltype(t), v.value, w.value>(op.st, a); }); });
     });
     return op.err;
   });
@@ -446,13 +424,12 @@ int pe_layernorm_bwd(pe_handle* h, long long rows, int c, int dtype, int x_type,
       a.add = add; a.ld_add = ld_add; a.dy = dy; a.ld_dy = ld_dy; a.out = dx; a.ld_out = ld_dx; a.gain = gain; a.stats_in = stats;
       a.part = params ? (float*)workspace : nullptr;
       a.rows = rows; a.c = c;
-      const int v = Width(c, e).take(a.x, ld_x, rows).take(dy, ld_dy, rows).take(add, ld_add, rows).take(dx, ld_dx, rows).v;
-      groups = ln_bwd_groups(rows, c, v);
+      const bool whole = Whole(c, e).take(a.x, ld_x, rows).take(dy, ld_dy, rows).take(add, ld_add, rows).take(dx, ld_dx, rows).ok;
+      groups = ln_bwd_groups(rows, c);
       const unsigned wg = (unsigned)groups;
       const double n = (double)rows * c;
       op.launch("layernorm bwd", "ln_op_bwd_kernel", 15 * n, n * e * (1 + (dx ? 1 : 0) + (add ? 1 : 0)) + (kept ? (double)ck_bytes(rows, c) : n * e), [&] {
-        if (dtype == PE_BF16) { if (v == 8) ln_bwd_run<bf16, 8>(op.st, a, wg); else if (v == 2) ln_bwd_run<bf16, 2>(op.st, a, wg); else ln_bwd_run<bf16, 1>(op.st, a, wg); }
-        else { if (v == 8) ln_bwd_run<float, 8>(op.st, a, wg); else if (v == 2) ln_bwd_run<float, 2>(op.st, a, wg); else ln_bwd_run<float, 1>(op.st, a, wg); }
+        type_dispatch(dtype, [&](auto t) { width_dispatch(c, whole, [&](auto v, auto w) { ln_bwd_run<decltype(t), v.value, w.value>(op.st, a, wg); }); });
       });
     }
     if (params && (groups || !accumulate)) columns_sum(op, "layernorm sums", (const float*)workspace, groups, 2 * c, d_gain, d_offset, c, accumulate != 0);
@@ -484,10 +461,15 @@ int pe_relpos_fwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
     if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "relative positions: the handle belongs to another device than the current one");
     a.table = table; a.add = add; a.out = out;
     const bool pair = p->layout == PE_RELPOS_PAIR;
-    const int v = Width(pair ? p->c : p->n_k, e).take(add, a.ld, 2).take(out, a.ld, 2).v;
+    const bool whole = Whole(pair ? p->c : p->n_k, e).take(add, a.ld, 2).take(out, a.ld, 2).ok;
     const double n = (double)p->n_q * p->n_k * p->c;
     op.launch("relpos fwd", pair ? "relpos_pair_fwd_kernel" : "relpos_heads_fwd_kernel", n, n * e * (add ? 2 : 1), [&] {
-      if (p->dtype == PE_BF16) rp_fwd_run<bf16>(op.st, a, p->layout, v); else rp_fwd_run<float>(op.st, a, p->layout, v);
+      type_dispatch(p->dtype, [&](auto t) {
+        using T = decltype(t);
+        if (!pair) width_dispatch(p->n_k, whole, [&](auto v, auto w) { rp_heads_fwd<T, v.value, w.value>(op.st, a); });
+        else if (whole) rp_pair_fwd<T, 8>(op.st, a);
+        else rp_pair_fwd<T, 1>(op.st, a);
+      });
     });
     return op.err;
   });
@@ -516,12 +498,15 @@ int pe_relpos_bwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
     const bool pair = p->layout == PE_RELPOS_PAIR;
     long long groups = 0;
     if (some) {
-      const int v = pair ? 1 : Width(p->n_k, e).take(d_out, a.ld, 2).v;
-      const int split = pair ? 0 : rp_heads_split(*p, v);
-      groups = pair ? rp_pair_groups(*p) : rp_heads_groups(*p, v);
+      const bool whole = Whole(p->n_k, e).take(d_out, a.ld, 2).ok;
+      groups = pair ? rp_pair_groups(*p) : rp_heads_groups(*p);
       const double n = (double)p->n_q * p->n_k * p->c;
       op.launch("relpos bwd", pair ? "relpos_pair_bwd_kernel" : "relpos_heads_bwd_kernel", n, n * e, [&] {
-        if (p->dtype == PE_BF16) rp_bwd_run<bf16>(op.st, h->device, a, p->layout, v, groups, split); else rp_bwd_run<float>(op.st, h->device, a, p->layout, v, groups, split);
+        type_dispatch(p->dtype, [&](auto t) {
+          using T = decltype(t);
+          if (pair) rp_pair_bwd_run<T>(op.st, h->device, a, groups);
+          else width_dispatch(p->n_k, whole, [&](auto v, auto w) { rp_heads_bwd<T, v.value, w.value>(op.st, h->device, a, rp_heads_split(*p)); });
+        });
       });
     }
     const int cols = a.nb * p->c;

@@ -76,6 +76,7 @@ template <int MODE> struct RpBuckets {
 
 // V neighbouring positions k of a lane.  far(): the bucket of all of them against q where it can be told without a look at each (all
 // beyond the outermost edges, or all of one other segment), otherwise -1.
+// (a ragged slot's elements that are its neighbour's among them)
 template <int V> struct RpLane {
   int pos[V], seg[V], least, most;
   bool one_seg;
@@ -146,21 +147,21 @@ __global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, in
 // HEADS, forward: a workgroup has one q, 256 V positions k and `heads` heads, whose table columns lie in LDS as [head][bucket]
 // (neighbouring distances are neighbouring banks).  A lane finds its V buckets once for all heads.
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V, int MODE>
+template <typename T, int V, bool WHOLE, int MODE>
 __global__ __launch_bounds__(256) void relpos_heads_fwd_kernel(const RpArgs a, int heads, int rows) {
   extern __shared__ float tab[];       // [heads][nb]
   __shared__ int edges[rp_lds_words(MODE)];
   const int h0 = blockIdx.z * heads, nh = min(heads, a.c - h0);
-  const int k = (blockIdx.x * 256 + threadIdx.x) * V;
+  const Slot<V, WHOLE> sl(blockIdx.x * 256 + threadIdx.x, a.n_k);
   RpBuckets<MODE>::fill(edges, a);
   for (int i = threadIdx.x; i < nh * a.nb; i += 256) {
     const int b = i / nh, h = i - b * nh;
     tab[h * a.nb + b] = a.table[(long long)b * a.c + h0 + h];
   }
   __syncthreads();
-  if (k >= a.n_k) return;
+  if (!sl.in) return;
   const RpBuckets<MODE> rb(edges, a);
-  const RpLane<V> at(a, k);
+  const RpLane<V> at(a, sl.at);
   const T* add = (const T*)a.add;
   T* out = (T*)a.out;
   for (int q = blockIdx.y * rows; q < min(a.n_q, (int)(blockIdx.y + 1) * rows); q++) {
@@ -175,9 +176,9 @@ __global__ __launch_bounds__(256) void relpos_heads_fwd_kernel(const RpArgs a, i
     }
     const bool all_far = V > 1 && __all(far >= 0);       // of the wave: one table entry per lane and head
     for (int h = 0; h < nh; h++) {
-      const long long o_at = ((long long)(h0 + h) * a.n_q + q) * a.ld + k;
+      const long long o_at = ((long long)(h0 + h) * a.n_q + q) * a.ld;
       Raw<T, V> o, ad;
-      if (add) ad = raw_load<T, V>(add + o_at);
+      if (add) ad = sl.load(add + o_at);
       float t[V];
       if (all_far) {
         const float one = tab[h * a.nb + far];
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(256) void relpos_heads_fwd_kernel(const RpArgs a, i
       }
 #pragma unroll
       for (int i = 0; i < V; i++) o.set(i, add ? ad.get(i) + t[i] : t[i]);
-      raw_store<T, V>(out + o_at, o);
+      sl.store(out + o_at, o);
     }
   }
 }
@@ -219,6 +220,8 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
   // a wave takes 64 positions, each as many behind the last as there are waves, so that every wave has its share of those whose bucket changes from one to the next: lane l
   // finds the place and the distance of the l-th
   int cnt, pq, pk, sq, sk, rlo, rhi;
+  const bool dense = a.ld == (long long)a.n_k * a.c;       // then the l-th lies l waves c elements behind the first
+  const T* first = nullptr;
   auto locate = [&](long long p) {
     cnt = (int)min((long long)64, (p1 - p + waves - 1) / waves);
     const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
@@ -228,11 +231,18 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
     sq = a.seg_q ? a.seg_q[q] : 0;
     sk = a.seg_q ? a.seg_k[k] : 0;
     const long long row = (long long)q * a.ld + (long long)k * a.c;            // the position's offset in d_out
+    first = g + p * a.c;
     rlo = (int)(uint32_t)(uint64_t)row;
     rhi = (int)(uint32_t)((uint64_t)row >> 32);
   };
   T next[U];
   auto load = [&]() {
+    if (S == 1 && dense && cnt == 64) {
+      const long long step = (long long)waves * a.c;
+#pragma unroll
+      for (int u = 0; u < U; u++) next[u] = first[u * step];
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const int l = u * S + sub;
@@ -255,23 +265,35 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
     for (int u = 0; u < U; u++) v[u] = next[u];
     p += 64LL * waves;
     if (p < p1) { locate(p); load(); }
-    int run = S == 1 ? __builtin_amdgcn_readlane(b, 0) : 0;                    // bucket of the run that is being added up
-    float sum = 0.0f;
+    if constexpr (S == 1) {
+      const uint64_t change = __ballot(b != __shfl_up(b, 1, 64));              // lane 0 compares with itself
+      int run = __builtin_amdgcn_readlane(b, 0);                               // bucket of the run that is being added up
+      float sum = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U; u++) {
-      const int l = u * S + sub;
-      if constexpr (S == 1) {
-        const int bb = __builtin_amdgcn_readlane(b, l);
-        if (l < now) {
-          if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
-          sum += (float)v[u];
-        }
-      } else {
-        const int bb = __shfl(b, l, 64);
+      for (int u0 = 0; u0 < U; u0 += 8) {
+        if (u0 + 8 <= now && ((change >> u0) & 255) == 0) {                    // most: all far from the outermost edges
+          float t = 0.0f;
+#pragma unroll
+          for (int u = u0; u < u0 + 8; u++) t += (float)v[u];
+          sum += t;
+        } else
+#pragma unroll
+          for (int u = u0; u < u0 + 8; u++) {
+            const int bb = __builtin_amdgcn_readlane(b, u);
+            if (u < now) {
+              if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
+              sum += (float)v[u];
+            }
+          }
+      }
+      lds_add(mine + run * 64, sum);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int l = u * S + sub, bb = __shfl(b, l, 64);
         if (l < now) lds_add(mine + bb * 64, (float)v[u]);
       }
     }
-    if constexpr (S == 1) lds_add(mine + run * 64, sum);
   }
   __syncthreads();
   // the waves' accumulators and the positions side by side, in a fixed order
@@ -292,7 +314,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 // [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).  Most lanes' positions are all farther than the outermost
 // edges, which their extremes tell: V elements are then one addition to LDS and no bucket is looked up.
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V, int U, int MODE>
+template <typename T, int V, bool WHOLE, int U, int MODE>
 __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -302,15 +324,16 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a) {
   for (int i = threadIdx.x; i < waves * a.nb * 64; i += blockDim.x) acc[i] = 0.0f;
   __syncthreads();
   const RpBuckets<MODE> rb(edges, a);
-  const int h = blockIdx.z, k = (blockIdx.x * 64 + lane) * V;
+  const int h = blockIdx.z;
+  const Slot<V, WHOLE> sl(blockIdx.x * 64 + lane, a.n_k);
   const int step = gridDim.y * waves;                      // rows between a wave's
-  if (k < a.n_k) {
-    RpLane<V> at(a, k);
-    const T* g = (const T*)a.d_out + (long long)h * a.n_q * a.ld + k;
+  if (sl.in) {
+    const RpLane<V> at(a, sl.at);
+    const T* g = (const T*)a.d_out + (long long)h * a.n_q * a.ld;
     Raw<T, V> next[U];
     auto fetch = [&](int q) {
 #pragma unroll
-      for (int u = 0; u < U; u++) next[u] = raw_load<T, V>(g + (long long)min(q + u * step, a.n_q - 1) * a.ld);
+      for (int u = 0; u < U; u++) next[u] = sl.load(g + (long long)min(q + u * step, a.n_q - 1) * a.ld);
     };
     int q = blockIdx.y * waves + wave;
     if (q < a.n_q) fetch(q);
@@ -326,16 +349,16 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a) {
         const int pq = a.pos_q[qu], sq = a.seg_q ? a.seg_q[qu] : 0;
         const int far = at.far(rb, pq, sq);
         if (far >= 0) {
-          float sum = v[u].get(0);
+          float sum = sl.has(0) ? v[u].get(0) : 0.0f;
 #pragma unroll
-          for (int i = 1; i < V; i++) sum += v[u].get(i);
+          for (int i = 1; i < V; i++) sum += sl.has(i) ? v[u].get(i) : 0.0f;
           lds_add(mine + far * 64, sum);
         } else {
           int b[V];
 #pragma unroll
           for (int i = 0; i < V; i++) b[i] = rb.of(pq, at.pos[i], sq, at.seg[i]);
 #pragma unroll
-          for (int i = 0; i < V; i++) lds_add(mine + b[i] * 64, v[u].get(i));
+          for (int i = 0; i < V; i++) lds_add(mine + b[i] * 64, sl.has(i) ? v[u].get(i) : 0.0f);
         }
       }
     }
