@@ -297,14 +297,17 @@ template <typename K> void allow_lds(K kern, int device, std::atomic<unsigned lo
   if (done.load() & bit) return;
   if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) done |= bit;
 }
-template <typename T, int S> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
+template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
   const int waves = rp_waves(a.nb);
   const long long n = (long long)a.n_q * a.n_k;
   rp_dispatch_few(a.mode, [&](auto m) {
-    static std::atomic<unsigned long long> done{0};
-    allow_lds(&relpos_pair_bwd_kernel<T, S, m.value>, device, done);
-    hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, m.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(64 * waves),
-                       rp_lds(a.nb, waves, m.value), st, a, (n + groups - 1) / groups);
+    auto launch = [&](auto near) {
+      static std::atomic<unsigned long long> done{0};
+      allow_lds(&relpos_pair_bwd_kernel<T, S, U, m.value, near.value>, device, done);
+      hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, U, m.value, near.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)),
+                         dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a, (n + groups - 1) / groups);
+    };
+    if ((double)a.n_q * (double)a.ld * sizeof(T) < 4e9) launch(std::true_type{}); else launch(std::false_type{});
   });
 }
 template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int device, const RpArgs& a, int split) {
@@ -318,10 +321,10 @@ template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int d
   });
 }
 template <typename T> void rp_pair_bwd_run(hipStream_t st, int device, const RpArgs& a, long long groups) {
-  if (a.c > 32) rp_pair_bwd<T, 1>(st, device, a, groups);
-  else if (a.c > 16) rp_pair_bwd<T, 2>(st, device, a, groups);
-  else if (a.c > 8) rp_pair_bwd<T, 4>(st, device, a, groups);
-  else rp_pair_bwd<T, 8>(st, device, a, groups);
+  if (a.c > 32) rp_pair_bwd<T, 1, 32>(st, device, a, groups);
+  else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, device, a, groups);
+  else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, device, a, groups);
+  else rp_pair_bwd<T, 8, 8>(st, device, a, groups);
 }
 
 }  // namespace
@@ -466,7 +469,9 @@ int pe_relpos_fwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
     op.launch("relpos fwd", pair ? "relpos_pair_fwd_kernel" : "relpos_heads_fwd_kernel", n, n * e * (add ? 2 : 1), [&] {
       type_dispatch(p->dtype, [&](auto t) {
         using T = decltype(t);
-        if (!pair) width_dispatch(p->n_k, whole, [&](auto v, auto w) { rp_heads_fwd<T, v.value, w.value>(op.st, a); });
+        // little to write: a position per lane, so that eight times the workgroups share it (1 x 8191 x 8: 3.7 us, by vectors 7.1)
+        if (!pair && n < (1 << 19)) rp_heads_fwd<T, 1, true>(op.st, a);
+        else if (!pair) width_dispatch(p->n_k, whole, [&](auto v, auto w) { rp_heads_fwd<T, v.value, w.value>(op.st, a); });
         else if (whole) rp_pair_fwd<T, 8>(op.st, a);
         else rp_pair_fwd<T, 1>(op.st, a);
       });

@@ -203,97 +203,104 @@ PE_DEV void lds_add(float* p, float v) { *p += v; }
 // PAIR, backward.  Lane = channel; a wave walks over positions and adds each to the LDS word [bucket][lane] of its own
 // accumulators.  Neighbouring positions of the same bucket (all that are farther than the outermost edges) are added in a register
 // first, which the whole wave decides together where it has one position at a time.  S positions share a wave where c <= 32.
-// blockIdx.y: slab of 64 channels (S = 1).  The loads of 64 positions are in flight per wave; lanes behind the last channel or position load a valid one,
+// blockIdx.y: slab of 64 channels (S = 1).  NEAR: offsets of d_out in bytes fit 32 bits, which
+// halves the instructions of a load.  The loads of a batch are in flight per wave; lanes behind the last channel or position load a valid one,
 // since a load under a condition is waited for by itself (2 bytes per lane and 126 us at 384 x 384 x 128).
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int S, int MODE>
+template <typename T, int S, int U, int MODE, bool NEAR>
 __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, long long per_group) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
-  constexpr int CL = 64 / S, U = 64 / S;       // lanes per position; loads per lane and 64 positions
+  constexpr int CL = 64 / S, BATCH = U * S;    // lanes per position; positions of a batch
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int sub = lane / CL, ch = blockIdx.y * 64 + lane % CL;
   int* edges = reinterpret_cast<int*>(acc + waves * a.nb * 64);
   float* mine = acc + wave * a.nb * 64 + lane;
   const T* g = (const T*)a.d_out + min(ch, a.c - 1);
+  const uint32_t ch_bytes = min(ch, a.c - 1) * (uint32_t)sizeof(T);
   const long long n = (long long)a.n_q * a.n_k;
   const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
-  // a wave takes 64 positions, each as many behind the last as there are waves, so that every wave has its share of those whose bucket changes from one to the next: lane l
-  // finds the place and the distance of the l-th
-  int cnt, pq, pk, sq, sk, rlo, rhi;
-  const bool dense = a.ld == (long long)a.n_k * a.c;       // then the l-th lies l waves c elements behind the first
-  const T* first = nullptr;
+  // A wave takes 64 positions, each as many behind the last as there are waves, so that every wave has its share of those whose bucket
+  // changes from one to the next.  Lane l finds the place and the distance of the l-th (lanes behind the last repeat it).
+  struct Places { int cnt, pq, pk, sq, sk, lo, hi; };
   auto locate = [&](long long p) {
-    cnt = (int)min((long long)64, (p1 - p + waves - 1) / waves);
+    Places r;
+    r.cnt = (int)min((long long)64, (p1 - p + waves - 1) / waves);
     const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
-    const int over = kk + min(lane, cnt - 1) * waves, dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
-    pq = a.pos_q[q];
-    pk = a.pos_k[k];
-    sq = a.seg_q ? a.seg_q[q] : 0;
-    sk = a.seg_q ? a.seg_k[k] : 0;
-    const long long row = (long long)q * a.ld + (long long)k * a.c;            // the position's offset in d_out
-    first = g + p * a.c;
-    rlo = (int)(uint32_t)(uint64_t)row;
-    rhi = (int)(uint32_t)((uint64_t)row >> 32);
+    const int over = kk + min(lane, r.cnt - 1) * waves, dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
+    r.pq = a.pos_q[q];
+    r.pk = a.pos_k[k];
+    r.sq = a.seg_q ? a.seg_q[q] : 0;
+    r.sk = a.seg_q ? a.seg_k[k] : 0;
+    const long long row = ((long long)q * a.ld + (long long)k * a.c) * (NEAR ? (int)sizeof(T) : 1);   // the position's offset in d_out
+    r.lo = (int)(uint32_t)(uint64_t)row;
+    r.hi = (int)(uint32_t)((uint64_t)row >> 32);
+    return r;
   };
   T next[U];
-  auto load = [&]() {
-    if (S == 1 && dense && cnt == 64) {
-      const long long step = (long long)waves * a.c;
-#pragma unroll
-      for (int u = 0; u < U; u++) next[u] = first[u * step];
-      return;
-    }
+  auto load = [&](int lo, int hi, int j) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int l = u * S + sub;
-      uint32_t lo, hi;
-      if constexpr (S == 1) { lo = __builtin_amdgcn_readlane(rlo, l); hi = __builtin_amdgcn_readlane(rhi, l); }
-      else { lo = (uint32_t)__shfl(rlo, l, 64); hi = (uint32_t)__shfl(rhi, l, 64); }
-      next[u] = g[(long long)(((uint64_t)hi << 32) | lo)];
+      const int l = j + u * S + sub;
+      const uint32_t x = S == 1 ? (uint32_t)__builtin_amdgcn_readlane(lo, l) : (uint32_t)__shfl(lo, l, 64);
+      if constexpr (NEAR) {
+        next[u] = *reinterpret_cast<const T*>((const char*)a.d_out + (x + ch_bytes));
+      } else {
+        const uint32_t y = S == 1 ? (uint32_t)__builtin_amdgcn_readlane(hi, l) : (uint32_t)__shfl(hi, l, 64);
+        next[u] = g[(long long)(((uint64_t)y << 32) | x)];
+      }
     }
   };
   long long p = p0 + wave;
-  if (p < p1) { locate(p); load(); }       // on their way while the accumulators are cleared, and the next 64 while these are added up
+  Places now;
+  if (p < p1) { now = locate(p); load(now.lo, now.hi, 0); }      // on their way while the accumulators are cleared
   RpBuckets<MODE>::fill(edges, a);
-  for (int i = threadIdx.x; i < waves * a.nb * 64; i += blockDim.x) acc[i] = 0.0f;
+  for (int i = threadIdx.x * 4; i < waves * a.nb * 64; i += blockDim.x * 4) *reinterpret_cast<f32x4*>(acc + i) = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   __syncthreads();
   const RpBuckets<MODE> rb(edges, a);
   while (p < p1) {
-    const int b = rb.of(pq, pk, sq, sk), now = cnt;
-    T v[U];
-#pragma unroll
-    for (int u = 0; u < U; u++) v[u] = next[u];
+    const int b = rb.of(now.pq, now.pk, now.sq, now.sk), cnt = now.cnt;
+    const uint64_t change = S == 1 ? __ballot(b != __shfl_up(b, 1, 64)) : 0;   // lane 0 compares with itself
+    int run = __builtin_amdgcn_readlane(b, 0);                                 // S = 1: bucket of the run that is being added up
+    float sum = 0.0f;
     p += 64LL * waves;
-    if (p < p1) { locate(p); load(); }
-    if constexpr (S == 1) {
-      const uint64_t change = __ballot(b != __shfl_up(b, 1, 64));              // lane 0 compares with itself
-      int run = __builtin_amdgcn_readlane(b, 0);                               // bucket of the run that is being added up
-      float sum = 0.0f;
+    Places then = now;
+    if (p < p1) then = locate(p);
+    // batches: while one is added up the next is on its way, the first of the next 64 behind the last.  The loop stays a loop: its
+    // 64 positions written out one after the other are 10 KB of instructions that every workgroup fetches anew.
+#pragma unroll 1
+    for (int j = 0; j < cnt; j += BATCH) {
+      T v[U];
 #pragma unroll
-      for (int u0 = 0; u0 < U; u0 += 8) {
-        if (u0 + 8 <= now && ((change >> u0) & 255) == 0) {                    // most: all far from the outermost edges
-          float t = 0.0f;
+      for (int u = 0; u < U; u++) v[u] = next[u];
+      const bool more = j + BATCH < cnt;
+      if (more || p < p1) load(more ? now.lo : then.lo, more ? now.hi : then.hi, more ? j + BATCH : 0);
+      if constexpr (S == 1) {
 #pragma unroll
-          for (int u = u0; u < u0 + 8; u++) t += (float)v[u];
-          sum += t;
-        } else
+        for (int u0 = 0; u0 < U; u0 += 8) {
+          if (j + u0 + 8 <= cnt && ((change >> (j + u0)) & 255) == 0) {        // most: all far from the outermost edges
+            sum += (((float)v[u0] + (float)v[u0 + 1]) + ((float)v[u0 + 2] + (float)v[u0 + 3])) +
+                   (((float)v[u0 + 4] + (float)v[u0 + 5]) + ((float)v[u0 + 6] + (float)v[u0 + 7]));
+          } else {
 #pragma unroll
-          for (int u = u0; u < u0 + 8; u++) {
-            const int bb = __builtin_amdgcn_readlane(b, u);
-            if (u < now) {
-              if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
-              sum += (float)v[u];
+            for (int u = u0; u < u0 + 8; u++) {
+              if (j + u < cnt) {
+                const int bb = __builtin_amdgcn_readlane(b, j + u);
+                if (bb != run) { lds_add(mine + run * 64, sum); run = bb; sum = 0.0f; }
+                sum += (float)v[u];
+              }
             }
           }
-      }
-      lds_add(mine + run * 64, sum);
-    } else {
+        }
+      } else {
 #pragma unroll
-      for (int u = 0; u < U; u++) {
-        const int l = u * S + sub, bb = __shfl(b, l, 64);
-        if (l < now) lds_add(mine + bb * 64, (float)v[u]);
+        for (int u = 0; u < U; u++) {
+          const int l = j + u * S + sub, bb = __shfl(b, l, 64);
+          if (l < cnt) lds_add(mine + bb * 64, (float)v[u]);
+        }
       }
     }
+    if constexpr (S == 1) lds_add(mine + run * 64, sum);
+    now = then;
   }
   __syncthreads();
   // the waves' accumulators and the positions side by side, in a fixed order
