@@ -41,7 +41,9 @@ def block_fwd_flops(d):
 
 
 def bench_trunk(args, torch, pe):
-    """Config 5: 4 extra-MSA blocks then 48 main blocks, per-block recompute, two streams."""
+    """Config 5: 4 extra-MSA blocks then 48 main blocks, two streams: every block's activations kept, or block inputs only and
+    per-block recompute (--recompute; --ckpt: with those inputs in 8 bits).  --recycle: a step also forms the trunk's inputs, the
+    previous step's representations through a layer norm and the relative positions, and takes their gradients."""
     from pe_inputs import dims_for, make_inputs
     from paper_2211_00235_amd.harness import to_dev
     de, me, _ = dims_for("extra_msa")
@@ -57,18 +59,23 @@ def bench_trunk(args, torch, pe):
     dmo, dzo = to_dev(im["d_msa_out"], bf), to_dev(im["d_pair_out"], bf)
     mo, zo, dex, dmi, dzi = (torch.empty_like(t) for t in (msa, pair, ex, msa, pair))
     dpar = torch.zeros_like(par)
-    keep = not args.recompute
-    ws = torch.empty(pe.stack_workspace_bytes(ne, de, nm, dm, keep=keep), dtype=torch.uint8, device="cuda")
+    keep = not (args.recompute or args.ckpt)
+    ws = torch.empty(pe.stack_workspace_bytes(ne, de, nm, dm, keep=keep, ckpt=args.ckpt), dtype=torch.uint8, device="cuda")
     h = pe.Handle()
+    if args.ckpt:
+        h.set_option(7, 1)      # PE_OPT_STACK_CKPT: block inputs in 8 bits
     if keep:
         h.set_option(5, 1)      # PE_OPT_STACK_KEEP_CTX: 288 GB hold every block's activations
     if args.no_overlap:
         h.set_option(6, 0)      # PE_OPT_STACK_OVERLAP off: no kernels of the next block before the current one's join
     sm, sp = torch.cuda.Stream(), torch.cuda.Stream()
 
-    def eager():
+    def trunk():
         pe.stack_fwd_bwd(h, ne, de, nm, dm, ex, msa, pair, exm, mm, pm, par, dmo, dzo, mo, zo, dex, dmi, dzi, dpar,
                          ws, sm, sp)
+    eager = trunk
+    if args.recycle:
+        eager = recycled_step(torch, pe, h, dm, msa, pair, dmi, dzi, trunk, sm)
     step = eager
     if args.graph:              # the whole trunk (about 9000 launches on two streams) as one HIP graph
         eager()
@@ -111,12 +118,41 @@ def bench_trunk(args, torch, pe):
         "config": {"workload": "trunk", "n_extra": ne, "n_main": nm, "streams": 2,
                    "launch": "hip graph replay" if args.graph else "eager",
                    "cross_block_overlap": bool(keep and not args.no_overlap),
-                   "recompute": "none (every block's activations kept)" if keep else "per block",
+                   "recompute": "none (every block's activations kept)" if keep else
+                                "per block, block inputs in 8 bits" if args.ckpt else "per block",
+                   "recycled_inputs": bool(args.recycle),
                    "workspace_gib": round(ws.numel() / 2 ** 30, 1)},
         "counted_tflops": flops / (ms * 1e-3) / 1e12,
         "bf16_mfma_peak_frac": flops / (ms * 1e-3) / 1e12 / PEAK_BF16_TFLOPS,
         "finite_outputs": bool(torch.isfinite(zo.float()).all().item() and torch.isfinite(dpar).all().item()),
         "cpu_baseline": cpu}))
+
+
+def recycled_step(torch, pe, h, d, msa, pair, d_msa, d_pair, trunk, sm):
+    """A step around `trunk`: msa[0] and pair are their embeddings plus the layer norm of the previous step's representations plus,
+    for the pair, the relative positions (distances clipped to 32); behind the trunk the gradients of both layer norms and of the table."""
+    r, cm, cz = d["r"], d["c_m"], d["c_z"]
+    f32 = dict(device="cuda")
+    prev_m, prev_z = torch.randn(r, cm, **f32).bfloat16(), torch.randn(r, r, cz, **f32).bfloat16()
+    base_m, base_z = msa[0].clone(), pair.clone()
+    gm, bm, gz, bz = torch.ones(cm, **f32), torch.zeros(cm, **f32), torch.ones(cz, **f32), torch.zeros(cz, **f32)
+    sm_, sz = torch.empty(r, 2, **f32), torch.empty(r * r, 2, **f32)
+    grads = [torch.empty(n, **f32) for n in (cm, cm, cz, cz)]
+    pos, edges = torch.arange(r, dtype=torch.int32, device="cuda"), torch.arange(-31, 33, dtype=torch.int32)
+    table, d_table = 0.1 * torch.randn(65, cz, **f32), torch.empty(65, cz, **f32)
+    byte = dict(dtype=torch.uint8, device="cuda")
+    wm, wz = (torch.empty(pe.layernorm_workspace_bytes(n, c), **byte) for n, c in ((r, cm), (r * r, cz)))
+    wt = torch.empty(pe.relpos_workspace_bytes(r, r, cz, 65), **byte)
+
+    def step():
+        pe.layernorm_fwd(h, prev_m, gm, bm, msa[0], add=base_m, stats=sm_, stream=sm)
+        pe.layernorm_fwd(h, prev_z, gz, bz, pair, add=base_z, stats=sz, stream=sm)
+        pe.relpos_fwd(h, pos, pos, edges, table, pair, add=pair, stream=sm)
+        trunk()
+        pe.relpos_bwd(h, pos, pos, edges, d_pair, d_table, wt, stream=sm)
+        pe.layernorm_bwd(h, d_pair, prev_z, sz, gz, None, grads[2], grads[3], wz, stream=sm)
+        pe.layernorm_bwd(h, d_msa[0], prev_m, sm_, gm, None, grads[0], grads[1], wm, stream=sm)
+    return step
 
 
 def kernel_symbol(name, dims):
@@ -155,6 +191,10 @@ def main():
     ap.add_argument("--recompute", action="store_true",
                     help="trunk workload: save block inputs only and recompute each block's forward in the backward "
                          "pass (the paper's memory-saving setting) instead of keeping every block's activations")
+    ap.add_argument("--ckpt", action="store_true",
+                    help="trunk workload: like --recompute, with the saved block inputs in 8 bits")
+    ap.add_argument("--recycle", action="store_true",
+                    help="trunk workload: a step also forms the recycled inputs and relative positions and their gradients")
     ap.add_argument("--graph", action="store_true",
                     help="capture one step (both streams) into a HIP graph once and time graph replays")
     ap.add_argument("--no-overlap", action="store_true",

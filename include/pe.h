@@ -168,9 +168,14 @@ int pe_handle_device(const pe_handle* h);   /* the device that was current in pe
  * mean waits for the pair branch (Section "Branch Parallelism": the MSA representation is final
  * before the outer product mean; the next row attention needs the new pair representation for
  * its bias only).  Results are bit-identical.  Measured without gain on one MI355X (the chip
- * is already full beside the pair branch's tail), hence off.                                 */
+ * is already full beside the pair branch's tail), hence off.
+ * PE_OPT_STACK_CKPT (default 0): 1 = pe_stack_fwd_bwd saves the block inputs that it keeps for
+ * the backward pass in 8 bits (pe_ckpt_pack: 33/64 of their bf16 size, 33/128 of fp32) and
+ * restores them in front of each block's recompute; pe_stack_workspace_bytes_ckpt bytes of
+ * workspace.  Outputs are bit-identical; cotangents and gradients are those of every block but
+ * the first and the last taken at its restored inputs.  Not together with PE_OPT_STACK_KEEP_CTX. */
 enum { PE_OPT_BRANCHES = 1, PE_OPT_SYNC_DEBUG = 2, PE_OPT_KERNEL_TIMING = 3, PE_OPT_SIDE_STREAMS = 4,
-       PE_OPT_STACK_KEEP_CTX = 5, PE_OPT_STACK_OVERLAP = 6 };
+       PE_OPT_STACK_KEEP_CTX = 5, PE_OPT_STACK_OVERLAP = 6, PE_OPT_STACK_CKPT = 7 };
 int pe_set_option(pe_handle* h, int option, int value);
 
 /* Per-kernel timing since the last collect, aggregated by launch label.
@@ -206,6 +211,8 @@ size_t pe_workspace_bytes(const pe_dims* d, int with_ctx);
 size_t pe_stack_workspace_bytes(int n_extra, const pe_dims* extra, int n_main, const pe_dims* main_);
 /* The same with PE_OPT_STACK_KEEP_CTX set (every block's ctx kept, no recompute). */
 size_t pe_stack_workspace_bytes_keep(int n_extra, const pe_dims* extra, int n_main, const pe_dims* main_);
+/* The same with PE_OPT_STACK_CKPT set (block inputs saved in 8 bits). */
+size_t pe_stack_workspace_bytes_ckpt(int n_extra, const pe_dims* extra, int n_main, const pe_dims* main_);
 
 /* Forward of one Parallel Evoformer block (Figure 1(c)).
  *   msa_in [s,r,c_m], pair_in [r,r,c_z]: inputs (dtype per dims), read only.
@@ -282,7 +289,8 @@ int pe_block_bwd(pe_handle* h, const pe_dims* dims,
  * dropped (its output cotangent is zero).  Block inputs are saved in the
  * forward pass and each block's forward is recomputed in the backward pass,
  * the last block's excepted, whose activations are still there (with
- * PE_OPT_STACK_KEEP_CTX every block's activations are kept instead).
+ * PE_OPT_STACK_KEEP_CTX every block's activations are kept instead, with
+ * PE_OPT_STACK_CKPT the saved inputs are held in 8 bits).
  *   params / d_params: the blocks' flat buffers back to back, extra first.
  *   msa_out, pair_out: final representations.  d_msa_out, d_pair_out: their
  *   cotangents.  d_extra_msa_in, d_msa_in, d_pair_in: overwritten.

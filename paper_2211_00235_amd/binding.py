@@ -74,6 +74,8 @@ def lib():
     L.pe_stack_workspace_bytes.restype = C.c_size_t
     L.pe_stack_workspace_bytes_keep.argtypes = [C.c_int, dp, C.c_int, dp]
     L.pe_stack_workspace_bytes_keep.restype = C.c_size_t
+    L.pe_stack_workspace_bytes_ckpt.argtypes = [C.c_int, dp, C.c_int, dp]
+    L.pe_stack_workspace_bytes_ckpt.restype = C.c_size_t
     L.pe_block_fwd.argtypes = [vp, dp, vp, vp, fp, fp, fp, vp, vp, vp, vp, C.c_size_t, vp, vp]
     L.pe_static_scratch_bytes.argtypes = []
     L.pe_static_scratch_bytes.restype = C.c_size_t
@@ -155,10 +157,12 @@ def workspace_bytes(d, with_ctx):
     return int(lib().pe_workspace_bytes(C.byref(_dims(d)), int(with_ctx)))
 
 
-def stack_workspace_bytes(n_extra, extra, n_main, main, keep=False):
+def stack_workspace_bytes(n_extra, extra, n_main, main, keep=False, ckpt=False):
+    """keep, ckpt: with the handle's option for kept activations (5) or for block inputs in 8 bits (7)."""
     e = C.byref(_dims(extra)) if extra is not None else None
     m = C.byref(_dims(main)) if main is not None else None
-    f = lib().pe_stack_workspace_bytes_keep if keep else lib().pe_stack_workspace_bytes
+    f = (lib().pe_stack_workspace_bytes_keep if keep else lib().pe_stack_workspace_bytes_ckpt if ckpt
+         else lib().pe_stack_workspace_bytes)
     return int(f(n_extra, e, n_main, m))
 
 

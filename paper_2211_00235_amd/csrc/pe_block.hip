@@ -19,6 +19,7 @@
 #include "pe_gemm.h"
 #include "pe_handle.h"
 #include "pe_layout.h"
+#include "pe_ops.h"
 #include "pe_pipe.h"
 #include "pe_rows.h"
 #include "pe_small.h"
@@ -2024,9 +2025,14 @@ struct StackPlan {
   size_t off_pair_saved, off_msa_saved, off_extra_saved, off_pp, off_block, block_bytes, total;
   bool keep;                            // every block's ctx is kept: nothing is recomputed
   size_t off_ctx, ctx_e, ctx_m;         // kept ctx slots: n_extra of ctx_e bytes, then n_main of ctx_m bytes
+  bool ckpt;                            // block inputs are saved in 8 bits, the two newest of each kind also as they are
+  size_t k_pair, k_msa, k_extra;        // bytes of one tensor in 8 bits
+  size_t off_two;                       // ckpt: two pair, two msa, two extra-msa tensors
 };
+enum StackMode { STACK_RECOMPUTE, STACK_KEEP, STACK_CKPT };
 static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
-static int make_stack_plan(int n_extra, const pe_dims* ex, int n_main, const pe_dims* mn, bool keep, StackPlan& sp) {
+static int make_stack_plan(int n_extra, const pe_dims* ex, int n_main, const pe_dims* mn, StackMode mode, StackPlan& sp) {
+  const bool keep = mode == STACK_KEEP;
   if (n_extra < 0 || n_main < 0 || n_extra + n_main < 1) return PE_ERR_ARG;
   if ((n_extra && !ex) || (n_main && !mn)) return PE_ERR_NULL;
   if (n_extra && pe_check_dims(ex)) return PE_ERR_DIMS;
@@ -2039,9 +2045,22 @@ static int make_stack_plan(int n_extra, const pe_dims* ex, int n_main, const pe_
   sp.n_extra = n_extra ? al256((size_t)ex->s * ex->r * ex->c_m * sp.E) : 0;
   int nb = n_extra + n_main;
   size_t off = 0;
-  sp.off_pair_saved = off; off += sp.n_pair * (size_t)(nb - 1);
-  sp.off_msa_saved = off; off += sp.n_msa * (size_t)(n_main > 0 ? n_main - 1 : 0);
-  sp.off_extra_saved = off; off += sp.n_extra * (size_t)n_extra;     // slot n_extra-1 = dropped final output
+  sp.ckpt = mode == STACK_CKPT;
+  sp.k_pair = sp.k_msa = sp.k_extra = sp.off_two = 0;
+  if (!sp.ckpt) {
+    sp.off_pair_saved = off; off += sp.n_pair * (size_t)(nb - 1);
+    sp.off_msa_saved = off; off += sp.n_msa * (size_t)(n_main > 0 ? n_main - 1 : 0);
+    sp.off_extra_saved = off; off += sp.n_extra * (size_t)n_extra;     // slot n_extra-1 = dropped final output
+  } else {
+    sp.k_pair = al256(pe_ckpt_bytes((long long)any->r * any->r, any->c_z));
+    sp.k_msa = n_main ? al256(pe_ckpt_bytes((long long)mn->s * mn->r, mn->c_m)) : 0;
+    sp.k_extra = n_extra ? al256(pe_ckpt_bytes((long long)ex->s * ex->r, ex->c_m)) : 0;
+    // the caller has the first block's inputs, and the last block's are never given up
+    sp.off_pair_saved = off; off += sp.k_pair * (size_t)std::max(0, nb - 2);
+    sp.off_msa_saved = off; off += sp.k_msa * (size_t)std::max(0, n_main - 2);
+    sp.off_extra_saved = off; off += sp.k_extra * (size_t)std::max(0, n_extra - (n_main ? 1 : 2));
+    sp.off_two = off; off += 2 * (sp.n_pair + sp.n_msa + sp.n_extra);
+  }
   sp.off_pp = off; off += 2 * (sp.n_pair + sp.n_msa + sp.n_extra);   // ping-pong cotangents
   sp.keep = keep;
   Plan pe_ = n_extra ? plan_for(*ex) : Plan{0, 0, 0, 0}, pm_ = n_main ? plan_for(*mn) : Plan{0, 0, 0, 0};
@@ -2065,11 +2084,35 @@ static int stack_impl(pe_handle* h, int n_extra, const pe_dims* ex, int n_main, 
   const int nb = n_extra + n_main;
   const long long pe_n = n_extra ? pe_param_count(ex) : 0, pm_n = n_main ? pe_param_count(mn) : 0;
   char* blockws = ws + sp.off_block;
-  auto pair_slot = [&](int b) -> char* { return ws + sp.off_pair_saved + sp.n_pair * (size_t)(b - 1); };   // input of block b>=1
+  // inputs of block b >= 1 (of main block k >= 1, of extra block b >= 1; extra block n_extra: the dropped final output)
+  char* two = ws + sp.off_two;
+  auto pair_slot = [&](int b) -> char* {
+    return sp.ckpt ? two + sp.n_pair * (size_t)(b & 1) : ws + sp.off_pair_saved + sp.n_pair * (size_t)(b - 1);
+  };
+  auto msa_slot = [&](int k) -> char* {
+    return sp.ckpt ? two + 2 * sp.n_pair + sp.n_msa * (size_t)(k & 1) : ws + sp.off_msa_saved + sp.n_msa * (size_t)(k - 1);
+  };
+  auto extra_slot = [&](int b) -> char* {
+    return sp.ckpt ? two + 2 * (sp.n_pair + sp.n_msa) + sp.n_extra * (size_t)(b & 1) : ws + sp.off_extra_saved + sp.n_extra * (size_t)(b - 1);
+  };
   auto x_in = [&](int b) -> const void* {
-    if (b < n_extra) return b == 0 ? extra_msa_in : (const void*)(ws + sp.off_extra_saved + sp.n_extra * (size_t)(b - 1));
+    if (b < n_extra) return b == 0 ? extra_msa_in : (const void*)extra_slot(b);
     int k = b - n_extra;
-    return k == 0 ? msa_in : (const void*)(ws + sp.off_msa_saved + sp.n_msa * (size_t)(k - 1));
+    return k == 0 ? msa_in : (const void*)msa_slot(k);
+  };
+  // 8-bit checkpoints (pe_ckpt_pack) of the inputs that the library holds, but for the last block's, which nothing overwrites before its
+  // backward pass.  Packed behind the block that wrote them, restored in front of the backward pass that reads them, on stream_msa: both
+  // streams have been joined there, and every block's entry makes stream_pair wait for it.
+  auto checkpoint = [&](int b, bool pack) -> int {
+    if (!sp.ckpt || b < 1 || b > nb - 2) return PE_OK;
+    const bool is_e = b < n_extra;
+    const pe_dims& d = is_e ? *ex : *mn;
+    int rc = ckpt_launch(h, sm, pack, d.dtype, pair_slot(b), ws + sp.off_pair_saved + sp.k_pair * (size_t)(b - 1), (long long)d.r * d.r, d.c_z);
+    const int k = is_e ? b : b - n_extra;      // inputs number 0 are the caller's
+    if (rc || k == 0) return rc;
+    return ckpt_launch(h, sm, pack, d.dtype, is_e ? extra_slot(k) : msa_slot(k),
+                       is_e ? ws + sp.off_extra_saved + sp.k_extra * (size_t)(k - 1) : ws + sp.off_msa_saved + sp.k_msa * (size_t)(k - 1),
+                       (long long)d.s * d.r, d.c_m);
   };
   auto z_in = [&](int b) -> const void* { return b == 0 ? pair_in : (const void*)pair_slot(b); };
   auto poff = [&](int b) -> long long { return b < n_extra ? pe_n * b : pe_n * n_extra + pm_n * (b - n_extra); };
@@ -2089,8 +2132,8 @@ static int stack_impl(pe_handle* h, int n_extra, const pe_dims* ex, int n_main, 
     const bool is_e = b < n_extra;
     const pe_dims& d = is_e ? *ex : *mn;
     void* xo;
-    if (is_e) xo = ws + sp.off_extra_saved + sp.n_extra * (size_t)b;
-    else xo = (b == nb - 1) ? msa_out : (void*)(ws + sp.off_msa_saved + sp.n_msa * (size_t)(b - n_extra));
+    if (is_e) xo = extra_slot(b + 1);
+    else xo = (b == nb - 1) ? msa_out : (void*)msa_slot(b - n_extra + 1);
     void* zo = (b == nb - 1) ? pair_out : (void*)pair_slot(b + 1);
     const bool chain = overlap_blocks && b + 1 < nb && d.variant == PE_VARIANT_PARALLEL &&
                        (b + 1 < n_extra ? ex : mn)->variant == PE_VARIANT_PARALLEL;
@@ -2101,6 +2144,7 @@ static int stack_impl(pe_handle* h, int n_extra, const pe_dims* ex, int n_main, 
     };
     int rc = block_fwd_impl<T>(h, d, x_in(b), z_in(b), is_e ? extra_mask : msa_mask, pair_mask, params + poff(b), xo, zo,
                                ctx_of(b), blockws, sp.block_bytes, sm, sp_, !sp.keep && b + 1 < nb, pre_done, chain ? &early : nullptr);
+    if (!rc) rc = checkpoint(b + 1, true);
     if (rc) return rc;
     pre_done = chain;
   }
@@ -2128,7 +2172,9 @@ static int stack_impl(pe_handle* h, int n_extra, const pe_dims* ex, int n_main, 
     void* dx_in;
     if (is_e) dx_in = (b == 0) ? d_extra_msa_in : (void*)de_pp[b & 1];
     else dx_in = (b == n_extra) ? d_msa_in : (void*)dm_pp[b & 1];
-    int rc = block_bwd_impl<T>(h, d, x_in(b), z_in(b), is_e ? extra_mask : msa_mask, pair_mask, params + poff(b),
+    int rc = checkpoint(b, false);
+    if (rc) return rc;
+    rc = block_bwd_impl<T>(h, d, x_in(b), z_in(b), is_e ? extra_mask : msa_mask, pair_mask, params + poff(b),
                                is_e ? de : dm, dz, dx_in, dz_in, d_params + poff(b), ctx_of(b), blockws, sp.block_bytes, sm,
                                sp_, b == nb - 1);
     if (rc) return rc;
@@ -2214,6 +2260,7 @@ int pe_create(pe_handle** out) {
   h->side_streams = 0;
   h->stack_keep = 0;
   h->stack_overlap = 0;
+  h->stack_ckpt = 0;
   h->side[0] = h->side[1] = nullptr;
   h->side_ev_next = 0;
   h->pair = nullptr;
@@ -2248,6 +2295,7 @@ int pe_set_option(pe_handle* h, int option, int value) {
   if (option == PE_OPT_KERNEL_TIMING) { h->timing = value ? 1 : 0; return PE_OK; }
   if (option == PE_OPT_STACK_KEEP_CTX) { h->stack_keep = value ? 1 : 0; return PE_OK; }
   if (option == PE_OPT_STACK_OVERLAP) { h->stack_overlap = value ? 1 : 0; return PE_OK; }
+  if (option == PE_OPT_STACK_CKPT) { h->stack_ckpt = value ? 1 : 0; return PE_OK; }
   if (option == PE_OPT_SIDE_STREAMS) {
     // Created on first use only: every extra stream competes for the process's few hardware
     // queues (4 by default), and two streams that share a queue serialise.
@@ -2464,12 +2512,17 @@ int pe_block_bwd(pe_handle* h, const pe_dims* dims, const void* msa_in, const vo
 
 size_t pe_stack_workspace_bytes(int n_extra, const pe_dims* extra, int n_main, const pe_dims* main_) {
   StackPlan sp;
-  if (make_stack_plan(n_extra, extra, n_main, main_, false, sp)) return 0;
+  if (make_stack_plan(n_extra, extra, n_main, main_, STACK_RECOMPUTE, sp)) return 0;
   return sp.total;
 }
 size_t pe_stack_workspace_bytes_keep(int n_extra, const pe_dims* extra, int n_main, const pe_dims* main_) {
   StackPlan sp;
-  if (make_stack_plan(n_extra, extra, n_main, main_, true, sp)) return 0;
+  if (make_stack_plan(n_extra, extra, n_main, main_, STACK_KEEP, sp)) return 0;
+  return sp.total;
+}
+size_t pe_stack_workspace_bytes_ckpt(int n_extra, const pe_dims* extra, int n_main, const pe_dims* main_) {
+  StackPlan sp;
+  if (make_stack_plan(n_extra, extra, n_main, main_, STACK_CKPT, sp)) return 0;
   return sp.total;
 }
 
@@ -2485,8 +2538,12 @@ int pe_stack_fwd_bwd(pe_handle* h, int n_extra, const pe_dims* extra, int n_main
     h->last_error = "pe_stack_fwd_bwd needs both branches (PE_OPT_BRANCHES = 3)";
     return PE_ERR_ARG;
   }
+  if (h->stack_keep && h->stack_ckpt) {
+    h->last_error = "pe_stack_fwd_bwd: PE_OPT_STACK_KEEP_CTX keeps what PE_OPT_STACK_CKPT would restore: set one of them";
+    return PE_ERR_ARG;
+  }
   StackPlan sp;
-  int rc = make_stack_plan(n_extra, extra, n_main, main_, h->stack_keep != 0, sp);
+  int rc = make_stack_plan(n_extra, extra, n_main, main_, h->stack_keep ? STACK_KEEP : h->stack_ckpt ? STACK_CKPT : STACK_RECOMPUTE, sp);
   if (rc) return rc;
   if (n_extra && (!extra_msa_in || !extra_msa_mask || !d_extra_msa_in)) return PE_ERR_NULL;
   if (n_main && (!msa_in || !msa_mask || !d_msa_out || !msa_out || !d_msa_in)) return PE_ERR_NULL;

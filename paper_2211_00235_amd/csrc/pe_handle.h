@@ -17,6 +17,7 @@ struct pe_handle {
   int side_streams;                 // PE_OPT_SIDE_STREAMS
   int stack_keep;                   // PE_OPT_STACK_KEEP_CTX
   int stack_overlap;                // PE_OPT_STACK_OVERLAP
+  int stack_ckpt;                   // PE_OPT_STACK_CKPT
   hipStream_t side[2];              // side stream of the MSA branch / of the pair branch
   hipEvent_t side_ev[32];           // ring of fork/join events
   int side_ev_next;

@@ -122,8 +122,8 @@ int ck_call(pe_handle* h, long long rows, int c, int dtype, const void* t, long 
   if (any_alias(rg, 2)) return op.refuse(PE_ERR_ALIAS, "checkpoint: tensor and checkpoint overlap");
   if (!op.device_ok()) return op.refuse(PE_ERR_ARG, "checkpoint: the handle belongs to another device than the current one");
   const bool whole = Whole(c, e).take(t, ld, rows).ok;
-  const double n = (double)rows * c, bytes = n * e + ck_bytes(rows, c);
-  op.launch(pack ? "ckpt pack" : "ckpt unpack", "ckpt_kernel", 2 * n, bytes, [&] {
+  const double n = (double)rows * c;
+  op.launch(pack ? "ckpt pack" : "ckpt unpack", "ckpt_kernel", 2 * n, n * e + ck_bytes(rows, c), [&] {
     if (pack) ck_run<true>(op.st, dtype, whole, t, ld, const_cast<void*>(ckpt), nullptr, rows, c);
     else ck_run<false>(op.st, dtype, whole, nullptr, ld, const_cast<void*>(ckpt), const_cast<void*>(t), rows, c);
   });
@@ -329,13 +329,13 @@ template <typename T> void rp_pair_bwd_run(hipStream_t st, int device, const RpA
 
 }  // namespace
 
-hipError_t ckpt_pack_launch(hipStream_t st, int dtype, const void* x, void* ckpt, long long rows, int c) {
-  ck_run<true>(st, dtype, true, x, c, ckpt, nullptr, rows, c);
-  return hipGetLastError();
-}
-hipError_t ckpt_unpack_launch(hipStream_t st, int dtype, const void* ckpt, void* y, long long rows, int c) {
-  ck_run<false>(st, dtype, true, nullptr, c, const_cast<void*>(ckpt), y, rows, c);
-  return hipGetLastError();
+int ckpt_launch(pe_handle* h, hipStream_t st, bool pack, int dtype, void* x, void* ckpt, long long rows, int c) {
+  OpCall op{h, st};
+  const double n = (double)rows * c;
+  op.launch(pack ? "ckpt pack" : "ckpt unpack", "ckpt_kernel", 2 * n, n * elem(dtype) + ck_bytes(rows, c), [&] {
+    if (pack) ck_run<true>(st, dtype, true, x, c, ckpt, nullptr, rows, c); else ck_run<false>(st, dtype, true, nullptr, c, ckpt, x, rows, c);
+  });
+  return op.err;
 }
 
 extern "C" {

@@ -116,3 +116,20 @@ def test_declared_in_the_header():
 def test_workspace_grows_with_what_it_holds(layout):
     small, large = (pe.relpos_workspace_bytes(n, n, 16, 33, layout) for n in (8, 512))
     assert 0 < small <= large
+
+
+@pytest.mark.parametrize("name", ["tiny", "af2_initial"])
+def test_trunk_workspace_with_8_bit_checkpoints(name):
+    """Saved inputs of the blocks between the first and the last take their 8-bit size; two of each kind are held as they are."""
+    from pe_inputs import CONFIGS
+    d = dict(CONFIGS[name][0])
+    up = lambda n: (n + 255) // 256 * 256
+    size = {0: 4, 1: 2}[d["dtype"]]
+    z, m = up(d["r"] ** 2 * d["c_z"] * size), up(d["s"] * d["r"] * d["c_m"] * size)
+    kz, km = up(pe.ckpt_bytes(d["r"] ** 2, d["c_z"])), up(pe.ckpt_bytes(d["s"] * d["r"], d["c_m"]))
+    for n in (1, 2, 3, 8, 48):
+        plain, ckpt = pe.stack_workspace_bytes(0, None, n, d), pe.stack_workspace_bytes(0, None, n, d, ckpt=True)
+        assert plain - ckpt == (n - 1) * (z + m) - max(0, n - 2) * (kz + km) - 2 * (z + m)
+    e = dict(CONFIGS["extra_msa"][0], r=d["r"], c_z=d["c_z"], dtype=d["dtype"])
+    assert 0 < pe.stack_workspace_bytes(4, e, 48, d, ckpt=True) < pe.stack_workspace_bytes(4, e, 48, d)
+    assert pe.stack_workspace_bytes(0, None, 0, None, ckpt=True) == 0
