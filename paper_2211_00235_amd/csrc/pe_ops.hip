@@ -210,10 +210,11 @@ long long rp_ld(const pe_relpos& p) { return p.ld ? p.ld : rp_row(p); }
 // take up to 4)
 int rp_waves(int nb) { return std::max(1, std::min(8, (int)(150 * 1024 / (nb * 256)))); }
 size_t rp_lds(int nb, int waves, int mode) { return (size_t)waves * nb * 256 + 4 * rp_lds_words(mode); }
-// PAIR: position groups.  Partial sums cost 8 bytes per group, bucket and channel: a group has at least 512 positions
+// PAIR: position groups, so many that with slabs of 64 channels there are 256 workgroups.  Partial sums cost 8 bytes per group, bucket
+// and channel: a group has at least 512 positions.
 long long rp_pair_groups(const pe_relpos& p) {
   const long long n = (long long)p.n_q * p.n_k;
-  return std::max<long long>(1, std::min<long long>(128, (n + 511) / 512));
+  return std::max<long long>(1, std::min<long long>(256 / ((p.c + 63) / 64), (n + 511) / 512));
 }
 // HEADS: 64 vectors of 8 positions k (fewer than 8: of one) per workgroup; so many workgroups share the rows q of those and of a head
 // that there are about 512, with a row per wave at least
@@ -291,11 +292,13 @@ template <typename T, int V, bool WHOLE> void rp_heads_fwd(hipStream_t st, const
                        (size_t)heads * a.nb * 4, st, a, heads, rows);
   });
 }
-// Dynamic LDS above 64 KB has to be allowed once per kernel and device
+// Dynamic LDS above 64 KB has to be allowed once per kernel and device; what is left of a CU's 160 KB is for static LDS
+constexpr int RP_LDS_MOST = 156 * 1024;
 template <typename K> void allow_lds(K kern, int device, std::atomic<unsigned long long>& done) {
   const unsigned long long bit = 1ull << (device & 63);
   if (done.load() & bit) return;
-  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess) done |= bit;
+  if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, RP_LDS_MOST) == hipSuccess) done |= bit;
+  else (void)hipGetLastError();      // the launch is refused then, and says so
 }
 template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
   const int waves = rp_waves(a.nb);
@@ -320,8 +323,25 @@ template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int d
                        dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a);
   });
 }
+// The matrix unit's kernel: up to 128 buckets, rows without gaps, more than 16 channels
+bool rp_pair_mm(const RpArgs& a) { return a.nb <= 128 && a.c > 16 && a.ld == (long long)a.n_k * a.c; }
+template <typename T, int NB> void rp_pair_bwd_mm(hipStream_t st, int device, const RpArgs& a, long long groups) {
+  const long long n = (long long)a.n_q * a.n_k;
+  rp_dispatch_few(a.mode, [&](auto m) {
+    static std::atomic<unsigned long long> done{0};
+    allow_lds(&relpos_pair_bwd_mm_kernel<T, NB, m.value>, device, done);
+    const size_t lds = (size_t)4 * NB * 32 * 64 * 4 + 512 + 4 * rp_lds_words(m.value);
+    hipLaunchKernelGGL((relpos_pair_bwd_mm_kernel<T, NB, m.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(512), lds, st,
+                       a, (n + groups - 1) / groups);
+  });
+}
 template <typename T> void rp_pair_bwd_run(hipStream_t st, int device, const RpArgs& a, long long groups) {
-  if (a.c > 32) rp_pair_bwd<T, 1, 32>(st, device, a, groups);
+  if (rp_pair_mm(a)) {
+    if (a.nb <= 32) rp_pair_bwd_mm<T, 1>(st, device, a, groups);
+    else if (a.nb <= 64) rp_pair_bwd_mm<T, 2>(st, device, a, groups);
+    else if (a.nb <= 96) rp_pair_bwd_mm<T, 3>(st, device, a, groups);
+    else rp_pair_bwd_mm<T, 4>(st, device, a, groups);
+  } else if (a.c > 32) rp_pair_bwd<T, 1, 32>(st, device, a, groups);
   else if (a.c > 16) rp_pair_bwd<T, 2, 16>(st, device, a, groups);
   else if (a.c > 8) rp_pair_bwd<T, 4, 16>(st, device, a, groups);
   else rp_pair_bwd<T, 8, 8>(st, device, a, groups);

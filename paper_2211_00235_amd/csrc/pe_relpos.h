@@ -316,6 +316,195 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
+// PAIR, backward, on the matrix unit: d_table[32 buckets][32 channels] += H D with H[bucket][position] = 1 where the position is in the
+// bucket, 0 elsewhere, and D = d_out[position][channel], 16 positions at a time.  The products are exact, sums fp32, and buckets in any
+// order cost the same; blocks of 32 buckets without a position among the 16 are left out.  A wave has 64 channels, two neighbouring ones
+// per lane (a load of the wave is two positions' 128 or 256 bytes; with one channel per lane the same products took twice the time),
+// and every 8th batch of 16 positions; its sums stay in registers.
+// 0 times infinity is NaN, so values that are not finite are taken out of D and added by themselves in the end.
+// ---------------------------------------------------------------------------------------------------------------------
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
+// Two channels of 8 positions of a lane: their products with H, given the positions' buckets as bytes
+template <typename T> struct RpPairs;
+template <> struct RpPairs<bf16> {
+  static constexpr int DEPTH = 4;         // batches in flight
+  uint32_t x[8];
+  PE_DEV void load(int i, const bf16* p) { x[i] = *reinterpret_cast<const u32_any*>(p); }
+  PE_DEV bool finite() const {
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
+    return m[0] < 0x7f80 && m[1] < 0x7f80;
+  }
+  PE_DEV void drop() {                    // what is not finite becomes 0
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      if ((x[i] & 0x7f80u) == 0x7f80u) x[i] &= 0xffff0000u;
+      if ((x[i] & 0x7f800000u) == 0x7f800000u) x[i] &= 0x0000ffffu;
+    }
+  }
+  PE_DEV void add(f32x16 (&acc)[2], uint2 bytes, uint32_t row) const {
+    const uint32_t y[2] = {bytes.x ^ (row * 0x01010101u), bytes.y ^ (row * 0x01010101u)};      // 0 where the bucket is this row's
+    union { uint32_t u[4]; bf16x8 f; } h, lo, hi;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const uint32_t two = __builtin_amdgcn_perm(0u, y[i >> 1], (i & 1) ? 0x0c030c02u : 0x0c010c00u);   // two bytes as 16-bit halves
+      const u16x2 off = __builtin_elementwise_min(__builtin_bit_cast(u16x2, two), u16x2{1, 1});
+      h.u[i] = __builtin_bit_cast(uint32_t, (u16x2)(u16x2{0x3f80, 0x3f80} - off * (uint16_t)0x3f80));   // 1.0 or 0
+      lo.u[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+      hi.u[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
+    }
+    Mma<bf16>::mma(acc[0], h.f, lo.f);
+    Mma<bf16>::mma(acc[1], h.f, hi.f);
+  }
+};
+template <> struct RpPairs<float> {
+  static constexpr int DEPTH = 2;
+  f32x2 x[8];
+  PE_DEV void load(int i, const float* p) { x[i] = *reinterpret_cast<const f32x2_any*>(p); }
+  PE_DEV bool finite() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = max(max(m, __float_as_uint(x[i][0]) & 0x7fffffffu), __float_as_uint(x[i][1]) & 0x7fffffffu);
+    return m < 0x7f800000u;
+  }
+  PE_DEV void drop() {
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+        if ((__float_as_uint(x[i][t]) & 0x7f800000u) == 0x7f800000u) x[i][t] = 0.0f;
+  }
+  PE_DEV void add(f32x16 (&acc)[2], uint2 bytes, uint32_t row) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const uint32_t b = ((i < 4 ? bytes.x : bytes.y) >> (8 * (i & 3))) & 255u;
+      const float h = b == row ? 1.0f : 0.0f;
+      Mma<float>::mma(acc[0], h, x[i][0]);
+      Mma<float>::mma(acc[1], h, x[i][1]);
+    }
+  }
+};
+
+// NB: blocks of 32 buckets.  LDS: [4][NB * 32][64] sums, 64 bytes of buckets per wave, the edges.  c >= 2.
+template <typename T, int NB, int MODE>
+__global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a, long long per_group) {
+  extern __shared__ float lds[];
+  constexpr int ROWS = NB * 32, D = RpPairs<T>::DEPTH, STEP = 8 * 16 * 4;      // positions that the 8 waves take in a round
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+  uint8_t* bytes = reinterpret_cast<uint8_t*>(lds + 4 * ROWS * 64) + wave * 64;
+  int* edges = reinterpret_cast<int*>(lds + 4 * ROWS * 64 + 128);
+  const int ch0 = blockIdx.y * 64, ch = min(ch0 + 2 * col, a.c - 2);           // lanes behind the last channels load those two
+  const long long n = (long long)a.n_q * a.n_k;
+  const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
+  const T* g = (const T*)a.d_out + ch;
+  // a wave's round: batches of 16 positions, 128 apart; lane l has the place of position l % 16 of batch l / 16
+  struct Places { int pq, pk, sq, sk; };
+  auto place_of = [&](long long p) { return min(p + 128 * (lane >> 4) + (lane & 15), n - 1); };
+  auto locate = [&](long long p) {
+    const long long q0 = p / a.n_k;
+    const long long over = place_of(p) - q0 * a.n_k;
+    const int dq = (int)((uint64_t)over < (1ull << 31) ? (uint32_t)over / (uint32_t)a.n_k : over / a.n_k), q = (int)q0 + dq, k = (int)(over - (long long)dq * a.n_k);
+    return Places{a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0};
+  };
+  RpPairs<T> v[D];
+  auto load = [&](RpPairs<T>& to, long long p) {             // positions p + 8 half + 0..7; those behind the end are the last one again
+    if (p >= p1) return;
+    if (p + 16 <= n) {
+      const T* at = g + (p + 8 * half) * a.c;
+#pragma unroll
+      for (int i = 0; i < 8; i++) to.load(i, at + (long long)i * a.c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) to.load(i, g + min(p + 8 * half + i, n - 1) * a.c);
+    }
+  };
+  long long p = p0 + 16 * wave;
+  Places now;
+  if (p < p1) {
+    now = locate(p);
+#pragma unroll
+    for (int j = 0; j < D; j++) load(v[j], p + 128 * j);
+  }
+  if constexpr (MODE != RP_DENSE) {
+    RpBuckets<MODE>::fill(edges, a);
+    __syncthreads();
+  }
+  const RpBuckets<MODE> rb(edges, a);
+  f32x16 acc[NB][2];
+#pragma unroll
+  for (int k = 0; k < NB; k++)
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) acc[k][t][e] = 0.0f;
+  bool odd = false;                                          // the wave has met a value that is not finite
+  for (; p < p1; p += STEP) {
+    const bool in = p + 128 * (lane >> 4) + (lane & 15) < p1;
+    const int b = in ? rb.of(now.pq, now.pk, now.sq, now.sk) : 255;          // 255: no row
+    bytes[lane] = (uint8_t)b;
+    uint64_t has[NB];
+#pragma unroll
+    for (int k = 0; k < NB; k++) has[k] = __ballot(in && (b >> 5) == k);
+    const long long next = p + STEP;
+    if (next < p1) now = locate(next);
+    RowsPiece::phase();                                      // the bytes are in LDS before they are read
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      RpPairs<T>& d = v[j % D];
+      if (p + 128 * j < p1) {
+        const uint2 bb = *reinterpret_cast<const uint2*>(bytes + 16 * j + 8 * half);
+        if (!__all(d.finite())) { odd = true; d.drop(); }
+#pragma unroll
+        for (int k = 0; k < NB; k++)
+          if ((has[k] >> (16 * j)) & 0xffff) d.add(acc[k], bb, 32 * k + col);
+      }
+      load(d, j + D < 4 ? p + 128 * (j + D) : next + 128 * (j + D - 4));
+    }
+    RowsPiece::phase();                                      // ... and read before the next ones
+  }
+  // the upper four waves' sums go to LDS, the lower four add theirs, then one sum over four
+  float* sums = lds + (wave & 3) * ROWS * 64;
+  auto at = [&](int k, int t, int e) { return (32 * k + acc_row(half, e)) * 64 + ch + t - ch0; };
+  // lanes behind the last channel have none of their own; of an odd number of channels the last lane has the second of its pair
+  const bool mine[2] = {ch == ch0 + 2 * col, ch == ch0 + 2 * col || ch0 + 2 * col == a.c - 1};
+  for (int up = 1; up >= 0; up--) {
+    if (wave >> 2 == up)
+#pragma unroll
+      for (int k = 0; k < NB; k++)
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+          if (mine[t])
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+              float* to = sums + at(k, t, e);
+              *to = up ? acc[k][t][e] : acc[k][t][e] + *to;
+            }
+    __syncthreads();
+  }
+  float* part = a.part + (long long)blockIdx.x * a.nb * a.c + ch0;
+  auto each = [&](auto&& f) {
+    for (int i = threadIdx.x; i < a.nb * 64; i += 512) if (ch0 + (i & 63) < a.c) f(i, part + (long long)(i >> 6) * a.c + (i & 63));
+  };
+  each([&](int i, float* to) { *to = (lds[i] + lds[i + ROWS * 64]) + (lds[i + 2 * ROWS * 64] + lds[i + 3 * ROWS * 64]); });
+  // values that are not finite: whatever their order, the sum is the same infinity or NaN, so the waves may add them to the same words
+  if (!__syncthreads_or(odd)) return;
+  for (int i = threadIdx.x; i < ROWS * 64; i += 512) lds[i] = 0.0f;
+  __syncthreads();
+  if (ch0 + lane < a.c)
+    for (p = p0 + wave; p < p1; p += 8) {
+      const float f = (float)((const T*)a.d_out)[p * a.c + ch0 + lane];
+      if ((__float_as_uint(f) & 0x7f800000u) != 0x7f800000u) continue;
+      const int q = (int)(p / a.n_k), k = (int)(p - (long long)q * a.n_k);
+      const int b = rb.of(a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0);
+      __hip_atomic_fetch_add(lds + b * 64 + lane, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+  __syncthreads();
+  each([&](int i, float* to) { *to += lds[i]; });
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
 // HEADS, backward.  Lane = V positions k; a wave walks over rows q of one head, U at a time, spread over all rows so that every wave has its
 // share of those near its positions (which cost several times the others), and adds to the LDS words
 // [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).  Most lanes' positions are all farther than the outermost

@@ -281,7 +281,7 @@ def rp_inputs(rng, n_q, n_k, edges, segs, c, spread=1.0):
 @pytest.mark.parametrize("n_q, n_k, c, edges, segs", [
     (1, 1, 1, [], False), (1, 1, 8, [0], True), (1, 700, 8, LOG, False), (300, 1, 16, CLIP, True), (33, 47, 128, CLIP, True), (64, 64, 64, LOG, False),
     (50, 50, 23, CLIP, False), (17, 1024, 4, LOG, True), (40, 56, 130, CLIP, True), (21, 88, 1, MANY, True), (9, 72, 40, MANY, False), (5, 16, 1024, CLIP, False),
-    (130, 264, 12, CLIP, False), (0, 5, 8, CLIP, False), (5, 0, 8, CLIP, True), (3, 2100, 33, [-2147483647, 0, 2147483647], False)])
+    (130, 264, 12, CLIP, False), (70, 70, 128, CLIP, True), (90, 41, 96, [3 * i for i in range(100)], True), (61, 77, 24, CLIP, False), (37, 45, 64, list(range(20)), False), (0, 5, 8, CLIP, False), (5, 0, 8, CLIP, True), (3, 2100, 33, [-2147483647, 0, 2147483647], False)])
 def test_relpos(h, layout, dt, n_q, n_k, c, edges, segs):
     rng = np.random.default_rng(n_q * 31 + n_k + c)
     pq, pk, ed, sq, sk, table, b, nb = rp_inputs(rng, n_q, n_k, edges, segs, c)
@@ -309,6 +309,25 @@ def test_relpos(h, layout, dt, n_q, n_k, c, edges, segs):
     d = rand(rng, shape, dt)
     pe.relpos_bwd(h, pq, pk, ed, d, dt_, ws, sq, sk, layout=layout)
     inside(dt_, ref.relpos_bwd(b, f64(d), nb, layout), (64 + n_q * n_k / 4) * U * ref.relpos_bwd(b, np.abs(f64(d)), nb, layout))
+
+
+@pytest.mark.parametrize("layout", ["pair", "heads"])
+@pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("n_q, n_k, c, edges", [(40, 64, 64, CLIP), (33, 50, 33, LOG), (21, 47, 20, CLIP), (40, 64, 8, CLIP), (17, 90, 48, MANY)])
+def test_relpos_gradients_that_are_not_finite(h, layout, dt, n_q, n_k, c, edges):
+    """An infinity or NaN shows in the sums of its own bucket and channel, and nowhere else."""
+    rng = np.random.default_rng(n_k)
+    pq, pk, ed, sq, sk, table, b, nb = rp_inputs(rng, n_q, n_k, edges, True, c)
+    shape = (n_q, n_k, c) if layout == "pair" else (c, n_q, n_k)
+    d = rng.integers(-8, 9, size=shape).astype(np.float64)
+    for i in range(24):
+        at = tuple(rng.integers(0, s) for s in shape)
+        d[at] = [np.inf, -np.inf, np.nan, np.inf][i % 4]
+    t, dtab = torch.from_numpy(d).to(dt).cuda(), torch.empty(nb, c, device="cuda")
+    pe.relpos_bwd(h, pq, pk, ed, t, dtab, bytes_(pe.relpos_workspace_bytes(n_q, n_k, c, nb, layout)), sq, sk, layout=layout)
+    want, got = ref.relpos_bwd(b, d, nb, layout), f64(dtab)
+    assert not np.isfinite(want).all() and np.isfinite(want).any()
+    assert np.array_equal(np.isnan(want), np.isnan(got)) and np.array_equal(want[~np.isnan(want)], got[~np.isnan(got)])
 
 
 @pytest.mark.parametrize("layout", ["pair", "heads"])
