@@ -71,7 +71,7 @@ template <int V, int LG> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>
 // fewer than 8 channels: 8, one group per row), so item / LG numbers the groups.  A wave takes 64 U consecutive items, all of its
 // loads in flight at once; their scales are 64 U / LG consecutive bytes, stored by as many lanes together.  `flat`: no gaps and
 // whole groups, one long row.  HBM-bound.
-template <typename T, int V, bool WHOLE, int U, bool PACK>
+template <typename T, int V, bool WHOLE, int U, bool PACK, bool NT>
 __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int8_t* codes, uint8_t* scales, T* y, long long rows,
                                                    int c, int per_row, int flat) {
   constexpr int LG = V == 8 ? 4 : 8;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int
     }
     const Slot<V, WHOLE> s(vec[u], c);
     if constexpr (PACK) {
-      v[u] = in[u] ? s.load(x + at[u]) : raw_zero<T, V>();
+      v[u] = in[u] ? s.template load<NT>(x + at[u]) : raw_zero<T, V>();
     } else if (in[u]) {
       cd[u] = codes_load(codes + code_at[u], s);
       sb[u] = scales[item / LG];

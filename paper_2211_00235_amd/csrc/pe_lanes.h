@@ -65,7 +65,21 @@ template <> struct Raw<float, 8> {
 };
 template <> struct Raw<float, 2> { f32x2 v; PE_DEV float get(int i) const { return v[i]; } PE_DEV void set(int i, float f) { v[i] = f; } };
 template <> struct Raw<float, 1> { float v; PE_DEV float get(int) const { return v; } PE_DEV void set(int, float f) { v = f; } };
-template <typename T, int V> PE_DEV Raw<T, V> raw_load(const T* p) { return *reinterpret_cast<const Raw<T, V>*>(p); }
+// NT: a non-temporal load, for tensors that are read once and much larger than what the caches keep: lines that such a stream allocates push
+// out what the kernels before have written, whose way to memory then stands in the stream's.
+template <bool NT, typename U> PE_DEV U load_as(const U* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p); else return *p;
+}
+template <typename T, int V, bool NT = false> PE_DEV Raw<T, V> raw_load(const T* p) {
+  Raw<T, V> r;
+  if constexpr (sizeof(Raw<T, V>) == 32) {
+    r.v[0] = load_as<NT>(reinterpret_cast<const f32x4*>(p));
+    r.v[1] = load_as<NT>(reinterpret_cast<const f32x4*>(p) + 1);
+  } else {
+    r.v = load_as<NT>(reinterpret_cast<const decltype(r.v)*>(p));
+  }
+  return r;
+}
 template <typename T, int V> PE_DEV void raw_store(T* p, const Raw<T, V>& r) { *reinterpret_cast<Raw<T, V>*>(p) = r; }
 template <typename T, int V> PE_DEV Raw<T, V> raw_zero() {
   Raw<T, V> r;
@@ -76,11 +90,11 @@ template <typename T, int V> PE_DEV Raw<T, V> raw_zero() {
 typedef bf16 bf16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
-PE_DEV Raw<bf16, 8> raw_load_any(const bf16* p) { Raw<bf16, 8> r; r.v = *reinterpret_cast<const bf16x8_any*>(p); return r; }
-PE_DEV Raw<float, 8> raw_load_any(const float* p) {
+template <bool NT> PE_DEV Raw<bf16, 8> raw_load_any(const bf16* p) { Raw<bf16, 8> r; r.v = load_as<NT>(reinterpret_cast<const bf16x8_any*>(p)); return r; }
+template <bool NT> PE_DEV Raw<float, 8> raw_load_any(const float* p) {
   Raw<float, 8> r;
-  r.v[0] = *reinterpret_cast<const f32x4_any*>(p);
-  r.v[1] = *reinterpret_cast<const f32x4_any*>(p + 4);
+  r.v[0] = load_as<NT>(reinterpret_cast<const f32x4_any*>(p));
+  r.v[1] = load_as<NT>(reinterpret_cast<const f32x4_any*>(p + 4));
   return r;
 }
 PE_DEV void raw_store_any(bf16* p, const Raw<bf16, 8>& r) { *reinterpret_cast<bf16x8_any*>(p) = r.v; }
@@ -100,8 +114,8 @@ template <int V, bool WHOLE> struct Slot {
     else { in = vec * V < c; at = min(vec * V, c - V); skip = vec * V - at; }
   }
   PE_DEV bool has(int i) const { return WHOLE || i >= skip; }
-  template <typename T> PE_DEV Raw<T, V> load(const T* row) const {
-    if constexpr (WHOLE) return raw_load<T, V>(row + at); else return raw_load_any(row + at);
+  template <bool NT = false, typename T> PE_DEV Raw<T, V> load(const T* row) const {
+    if constexpr (WHOLE) return raw_load<T, V, NT>(row + at); else return raw_load_any<NT>(row + at);
   }
   template <typename T> PE_DEV void store(T* row, const Raw<T, V>& r) const {
     if constexpr (WHOLE) raw_store<T, V>(row + at, r);

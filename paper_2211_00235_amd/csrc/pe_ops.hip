@@ -81,6 +81,13 @@ template <typename F> void width_dispatch(long long c, bool whole, F&& f) {
   else if (whole) f(std::integral_constant<int, 8>{}, std::true_type{});
   else f(std::integral_constant<int, 8>{}, std::false_type{});
 }
+// Non-temporal loads of a tensor that a call reads once: from 32 MB on (an eighth of the memory-side cache).  With and without, us:
+// relpos pair backward 17 MB of gradients 12.9 and 11.5, 38 MB 14.8 and 17.4, 268 MB 49 and 78; packing and restoring 17 MB 13.5 and
+// 13.1, 252 MB 134 and 141.  Layer norm stays without: its backward pass finds part of what the forward pass has read (29 MB fp32, both passes,
+// 38.2 and 34.5, 67 MB bf16 90.1 and 87.6).
+template <typename F> void stream_dispatch(double bytes, F&& f) {
+  if (bytes >= 32e6) f(std::true_type{}); else f(std::false_type{});
+}
 template <typename F> void type_dispatch(int dtype, F&& f) {
   if (dtype == PE_BF16) f(bf16{}); else f(float{});
 }
@@ -102,8 +109,10 @@ template <bool PACK> void ck_run(hipStream_t st, int dtype, bool whole, const vo
       constexpr int V = v.value, U = 4;
       const int per_row = V == 8 ? (int)ck_groups(c) * 4 : 8;
       const long long items = rows * per_row, blocks = (items + 256 * U - 1) / (256 * U);
-      hipLaunchKernelGGL((ckpt_kernel<T, V, w.value, U, PACK>), dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
-                         (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row, (int)(c % CK_GROUP == 0 && (ld == c || rows == 1)));
+      stream_dispatch(PACK ? (double)rows * c * sizeof(T) : 0.0, [&](auto nt) {
+        hipLaunchKernelGGL((ckpt_kernel<T, V, w.value, U, PACK, nt.value>), dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
+                           (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row, (int)(c % CK_GROUP == 0 && (ld == c || rows == 1)));
+      });
     });
   });
 }
@@ -302,13 +311,12 @@ template <typename K> void allow_lds(K kern, int device, std::atomic<unsigned lo
 }
 template <typename T, int S, int U> void rp_pair_bwd(hipStream_t st, int device, const RpArgs& a, long long groups) {
   const int waves = rp_waves(a.nb);
-  const long long n = (long long)a.n_q * a.n_k;
   rp_dispatch_few(a.mode, [&](auto m) {
     auto launch = [&](auto near) {
       static std::atomic<unsigned long long> done{0};
       allow_lds(&relpos_pair_bwd_kernel<T, S, U, m.value, near.value>, device, done);
       hipLaunchKernelGGL((relpos_pair_bwd_kernel<T, S, U, m.value, near.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)),
-                         dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a, (n + groups - 1) / groups);
+                         dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a);
     };
     if ((double)a.n_q * (double)a.ld * sizeof(T) < 4e9) launch(std::true_type{}); else launch(std::false_type{});
   });
@@ -317,22 +325,24 @@ template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int d
   constexpr int U = V == 8 ? 4 : 8;
   const int waves = rp_waves(a.nb);
   rp_dispatch(a.mode, (long long)V * a.n_q < 10LL * split * waves, [&](auto m) {
-    static std::atomic<unsigned long long> done{0};
-    allow_lds(&relpos_heads_bwd_kernel<T, V, WHOLE, U, m.value>, device, done);
-    hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, WHOLE, U, m.value>), dim3((unsigned)(((a.n_k + V - 1) / V + 63) / 64), (unsigned)split, (unsigned)a.c),
-                       dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a);
+    stream_dispatch((double)a.n_q * a.n_k * a.c * sizeof(T), [&](auto nt) {
+      static std::atomic<unsigned long long> done{0};
+      allow_lds(&relpos_heads_bwd_kernel<T, V, WHOLE, U, m.value, nt.value>, device, done);
+      hipLaunchKernelGGL((relpos_heads_bwd_kernel<T, V, WHOLE, U, m.value, nt.value>), dim3((unsigned)(((a.n_k + V - 1) / V + 63) / 64), (unsigned)split, (unsigned)a.c),
+                         dim3(64 * waves), rp_lds(a.nb, waves, m.value), st, a);
+    });
   });
 }
-// The matrix unit's kernel: up to 128 buckets, rows without gaps, more than 16 channels
-bool rp_pair_mm(const RpArgs& a) { return a.nb <= 128 && a.c > 16 && a.ld == (long long)a.n_k * a.c; }
+// The matrix unit's kernel: up to 128 buckets, rows without gaps, more than 16 channels, a batch of positions at least
+bool rp_pair_mm(const RpArgs& a) { return a.nb <= 128 && a.c > 16 && a.ld == (long long)a.n_k * a.c && (long long)a.n_q * a.n_k >= 16; }
 template <typename T, int NB> void rp_pair_bwd_mm(hipStream_t st, int device, const RpArgs& a, long long groups) {
-  const long long n = (long long)a.n_q * a.n_k;
   rp_dispatch_few(a.mode, [&](auto m) {
-    static std::atomic<unsigned long long> done{0};
-    allow_lds(&relpos_pair_bwd_mm_kernel<T, NB, m.value>, device, done);
-    const size_t lds = (size_t)4 * NB * 32 * 64 * 4 + 512 + 4 * rp_lds_words(m.value);
-    hipLaunchKernelGGL((relpos_pair_bwd_mm_kernel<T, NB, m.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(512), lds, st,
-                       a, (n + groups - 1) / groups);
+    stream_dispatch((double)a.n_q * a.n_k * a.c * sizeof(T), [&](auto nt) {
+      static std::atomic<unsigned long long> done{0};
+      allow_lds(&relpos_pair_bwd_mm_kernel<T, NB, m.value, nt.value>, device, done);
+      const size_t lds = (size_t)4 * NB * 32 * 64 * 4 + 512 + 4 * rp_lds_words(m.value);
+      hipLaunchKernelGGL((relpos_pair_bwd_mm_kernel<T, NB, m.value, nt.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(512), lds, st, a);
+    });
   });
 }
 template <typename T> void rp_pair_bwd_run(hipStream_t st, int device, const RpArgs& a, long long groups) {

@@ -208,7 +208,7 @@ PE_DEV void lds_add(float* p, float v) { *p += v; }
 // since a load under a condition is waited for by itself (2 bytes per lane and 126 us at 384 x 384 x 128).
 // ---------------------------------------------------------------------------------------------------------------------
 template <typename T, int S, int U, int MODE, bool NEAR>
-__global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, long long per_group) {
+__global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
   constexpr int CL = 64 / S, BATCH = U * S;    // lanes per position; positions of a batch
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -218,13 +218,14 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
   const T* g = (const T*)a.d_out + min(ch, a.c - 1);
   const uint32_t ch_bytes = min(ch, a.c - 1) * (uint32_t)sizeof(T);
   const long long n = (long long)a.n_q * a.n_k;
-  const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
+  const long long p1 = n, step = 64LL * waves * gridDim.x;        // the workgroups take 64 positions per wave in turn
   // A wave takes 64 positions, each as many behind the last as there are waves, so that every wave has its share of those whose bucket
   // changes from one to the next.  Lane l finds the place and the distance of the l-th (lanes behind the last repeat it).
   struct Places { int cnt, pq, pk, sq, sk, lo, hi; };
   auto locate = [&](long long p) {
     Places r;
-    r.cnt = (int)min((long long)64, (p1 - p + waves - 1) / waves);
+    p = min(p, p1 - 1);                                      // behind the end: any place
+    r.cnt = (int)min((long long)64, (p1 - p + waves - 1) / waves);      // p: the first of the wave's
     const int q0 = (int)(p / a.n_k), kk = (int)(p - (long long)q0 * a.n_k);    // of the first position
     const int over = kk + min(lane, r.cnt - 1) * waves, dq = over / a.n_k, q = q0 + dq, k = over - dq * a.n_k;
     r.pq = a.pos_q[q];
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
       }
     }
   };
-  long long p = p0 + wave;
+  long long p = 64LL * waves * blockIdx.x + wave;
   Places now;
   if (p < p1) { now = locate(p); load(now.lo, now.hi, 0); }      // on their way while the accumulators are cleared
   RpBuckets<MODE>::fill(edges, a);
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
     const uint64_t change = S == 1 ? __ballot(b != __shfl_up(b, 1, 64)) : 0;   // lane 0 compares with itself
     int run = __builtin_amdgcn_readlane(b, 0);                                 // S = 1: bucket of the run that is being added up
     float sum = 0.0f;
-    p += 64LL * waves;
+    p += step;
     Places then = now;
     if (p < p1) then = locate(p);
     // batches: while one is added up the next is on its way, the first of the next 64 behind the last.  The loop stays a loop: its
@@ -321,7 +322,8 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a, lo
 // order cost the same; blocks of 32 buckets without a position among the 16 are left out.  A wave has 64 channels, two neighbouring ones
 // per lane (a load of the wave is two positions' 128 or 256 bytes; with one channel per lane the same products took twice the time),
 // and every 8th batch of 16 positions; its sums stay in registers.
-// 0 times infinity is NaN, so values that are not finite are taken out of D and added by themselves in the end.
+// 0 times infinity is NaN: a value that is not finite makes sums of other buckets NaN too, and a workgroup that finds such a sum in the
+// end forms all of its sums again without products.
 // ---------------------------------------------------------------------------------------------------------------------
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32_any __attribute__((aligned(2)));
@@ -330,20 +332,7 @@ template <typename T> struct RpPairs;
 template <> struct RpPairs<bf16> {
   static constexpr int DEPTH = 4;         // batches in flight
   uint32_t x[8];
-  PE_DEV void load(int i, const bf16* p) { x[i] = *reinterpret_cast<const u32_any*>(p); }
-  PE_DEV bool finite() const {
-    u16x2 m = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
-    return m[0] < 0x7f80 && m[1] < 0x7f80;
-  }
-  PE_DEV void drop() {                    // what is not finite becomes 0
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      if ((x[i] & 0x7f80u) == 0x7f80u) x[i] &= 0xffff0000u;
-      if ((x[i] & 0x7f800000u) == 0x7f800000u) x[i] &= 0x0000ffffu;
-    }
-  }
+  template <bool NT> PE_DEV void load(int i, const bf16* p) { x[i] = load_as<NT>(reinterpret_cast<const u32_any*>(p)); }
   PE_DEV void add(f32x16 (&acc)[2], uint2 bytes, uint32_t row) const {
     const uint32_t y[2] = {bytes.x ^ (row * 0x01010101u), bytes.y ^ (row * 0x01010101u)};      // 0 where the bucket is this row's
     union { uint32_t u[4]; bf16x8 f; } h, lo, hi;
@@ -362,20 +351,7 @@ template <> struct RpPairs<bf16> {
 template <> struct RpPairs<float> {
   static constexpr int DEPTH = 2;
   f32x2 x[8];
-  PE_DEV void load(int i, const float* p) { x[i] = *reinterpret_cast<const f32x2_any*>(p); }
-  PE_DEV bool finite() const {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i++) m = max(max(m, __float_as_uint(x[i][0]) & 0x7fffffffu), __float_as_uint(x[i][1]) & 0x7fffffffu);
-    return m < 0x7f800000u;
-  }
-  PE_DEV void drop() {
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-#pragma unroll
-      for (int t = 0; t < 2; t++)
-        if ((__float_as_uint(x[i][t]) & 0x7f800000u) == 0x7f800000u) x[i][t] = 0.0f;
-  }
+  template <bool NT> PE_DEV void load(int i, const float* p) { x[i] = load_as<NT>(reinterpret_cast<const f32x2_any*>(p)); }
   PE_DEV void add(f32x16 (&acc)[2], uint2 bytes, uint32_t row) const {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -387,46 +363,55 @@ template <> struct RpPairs<float> {
   }
 };
 
-// NB: blocks of 32 buckets.  LDS: [4][NB * 32][64] sums, 64 bytes of buckets per wave, the edges.  c >= 2.
-template <typename T, int NB, int MODE>
-__global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a, long long per_group) {
+// NB: blocks of 32 buckets.  LDS: [4][NB * 32][64] sums, 64 bytes of buckets per wave, the edges.  c >= 2, n_q n_k >= 16.
+template <typename T, int NB, int MODE, bool NT>
+__global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a) {
   extern __shared__ float lds[];
-  constexpr int ROWS = NB * 32, D = RpPairs<T>::DEPTH, STEP = 8 * 16 * 4;      // positions that the 8 waves take in a round
+  constexpr int ROWS = NB * 32, D = RpPairs<T>::DEPTH;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   uint8_t* bytes = reinterpret_cast<uint8_t*>(lds + 4 * ROWS * 64) + wave * 64;
   int* edges = reinterpret_cast<int*>(lds + 4 * ROWS * 64 + 128);
   const int ch0 = blockIdx.y * 64, ch = min(ch0 + 2 * col, a.c - 2);           // lanes behind the last channels load those two
   const long long n = (long long)a.n_q * a.n_k;
-  const long long p0 = (long long)blockIdx.x * per_group, p1 = min(n, p0 + per_group);
-  const T* g = (const T*)a.d_out + ch;
-  // a wave's round: batches of 16 positions, 128 apart; lane l has the place of position l % 16 of batch l / 16
-  struct Places { int pq, pk, sq, sk; };
-  auto place_of = [&](long long p) { return min(p + 128 * (lane >> 4) + (lane & 15), n - 1); };
-  auto locate = [&](long long p) {
-    const long long q0 = p / a.n_k;
-    const long long over = place_of(p) - q0 * a.n_k;
-    const int dq = (int)((uint64_t)over < (1ull << 31) ? (uint32_t)over / (uint32_t)a.n_k : over / a.n_k), q = (int)q0 + dq, k = (int)(over - (long long)dq * a.n_k);
-    return Places{a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0};
-  };
-  RpPairs<T> v[D];
-  auto load = [&](RpPairs<T>& to, long long p) {             // positions p + 8 half + 0..7; those behind the end are the last one again
-    if (p >= p1) return;
-    if (p + 16 <= n) {
-      const T* at = g + (p + 8 * half) * a.c;
-#pragma unroll
-      for (int i = 0; i < 8; i++) to.load(i, at + (long long)i * a.c);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; i++) to.load(i, g + min(p + 8 * half + i, n - 1) * a.c);
-    }
-  };
+  const int* seg_q = a.seg_q ? a.seg_q : a.pos_q;            // without segments: loaded and not used
+  const int* seg_k = a.seg_q ? a.seg_k : a.pos_k;
+  // The workgroups take 128 positions (16 per wave) in turn, so that all of them read neighbouring memory: with a range of its own for
+  // each, all moved through the memory's channels together (1024 x 1024 x 128 MM_RANGE us).  A wave's round is four of its batches; lane l has
+  // the place of position l % 16 of batch l / 16, and steps from round to round without a division.
+  const int apart = 128 * gridDim.x, step = 4 * apart;
+  const long long p0 = 128LL * blockIdx.x;
   long long p = p0 + 16 * wave;
-  Places now;
-  if (p < p1) {
-    now = locate(p);
-#pragma unroll
-    for (int j = 0; j < D; j++) load(v[j], p + 128 * j);
+  const int mine_at = apart * (lane >> 4) + (lane & 15);
+  int q, k;
+  {
+    const long long q0 = min(p, n - 1) / a.n_k, over = min(p, n - 1) - q0 * a.n_k + mine_at;
+    const int dq = (int)(over / a.n_k);
+    q = (int)q0 + dq;
+    k = (int)(over - (long long)dq * a.n_k);
   }
+  const int step_q = step / a.n_k, step_k = step % a.n_k;
+  struct Places { int pq, pk, sq, sk; };
+  auto places = [&]() {                                      // q may be behind the end: any place then
+    const int r = min(q, a.n_q - 1);
+    return Places{a.pos_q[r], a.pos_k[k], seg_q[r], seg_k[k]};
+  };
+  // A batch's positions, of which lane half h has 8 h + 0..7.  A batch that reaches behind the end is the last 16 positions instead.  Every
+  // round issues the same loads, needed or not: after a load under a condition the compiler waits for all that came before it, and
+  // the batches in flight are lost.
+  RpPairs<T> v[D];
+  const uint32_t lane_bytes = (uint32_t)(8 * half * a.c + ch) * (uint32_t)sizeof(T);
+  auto load = [&](RpPairs<T>& to, long long p) {
+    const char* at = (const char*)a.d_out + min(p, n - 16) * a.c * (long long)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 8; i++) to.template load<NT>(i, reinterpret_cast<const T*>(at + (long long)(i * a.c) * (int)sizeof(T) + lane_bytes));
+  };
+  // requested in the order in which the loop requests them, which the compiler is held to: what it waits for at the top of a round
+  // is what has to be there in every round (with the places requested last it waited for all loads, every round)
+  Places now = places();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < D; j++) load(v[j], p + apart * j);
+  asm volatile("" ::: "memory");
   if constexpr (MODE != RP_DENSE) {
     RpBuckets<MODE>::fill(edges, a);
     __syncthreads();
@@ -439,31 +424,41 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a,
     for (int t = 0; t < 2; t++)
 #pragma unroll
       for (int e = 0; e < 16; e++) acc[k][t][e] = 0.0f;
-  bool odd = false;                                          // the wave has met a value that is not finite
-  for (; p < p1; p += STEP) {
-    const bool in = p + 128 * (lane >> 4) + (lane & 15) < p1;
-    const int b = in ? rb.of(now.pq, now.pk, now.sq, now.sk) : 255;          // 255: no row
-    bytes[lane] = (uint8_t)b;
+  for (; p < n; p += step) {
+    const bool in = p + mine_at < n;
+    const int b = rb.of(now.pq, now.pk, a.seg_q ? now.sq : 0, a.seg_q ? now.sk : 0);
+    const long long behind = p + apart * (lane >> 4) + 16 - n;
+    const int shift = behind > 0 ? (int)min(behind, 16LL) : 0;                 // places that the batch was moved down by
+    bytes[lane] = 255;                                       // no row
+    RowsPiece::phase();
+    if (in && (lane & 15) + shift < 16) bytes[lane + shift] = (uint8_t)b;
     uint64_t has[NB];
 #pragma unroll
     for (int k = 0; k < NB; k++) has[k] = __ballot(in && (b >> 5) == k);
-    const long long next = p + STEP;
-    if (next < p1) now = locate(next);
+    q += step_q;
+    k += step_k;
+    if (k >= a.n_k) { k -= a.n_k; q++; }
+    now = places();
+    asm volatile("" ::: "memory");
     RowsPiece::phase();                                      // the bytes are in LDS before they are read
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       RpPairs<T>& d = v[j % D];
-      if (p + 128 * j < p1) {
-        const uint2 bb = *reinterpret_cast<const uint2*>(bytes + 16 * j + 8 * half);
-        if (!__all(d.finite())) { odd = true; d.drop(); }
+      const uint2 bb = *reinterpret_cast<const uint2*>(bytes + 16 * j + 8 * half);
 #pragma unroll
-        for (int k = 0; k < NB; k++)
-          if ((has[k] >> (16 * j)) & 0xffff) d.add(acc[k], bb, 32 * k + col);
-      }
-      load(d, j + D < 4 ? p + 128 * (j + D) : next + 128 * (j + D - 4));
+      for (int k = 0; k < NB; k++)
+        if ((has[k] >> (16 * j)) & 0xffff) d.add(acc[k], bb, 32 * k + col);
+      load(d, p + apart * (j + D));
     }
     RowsPiece::phase();                                      // ... and read before the next ones
   }
+  bool odd = false;
+#pragma unroll
+  for (int k = 0; k < NB; k++)
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) odd = odd || (__float_as_uint(acc[k][t][e]) & 0x7f800000u) == 0x7f800000u;
   // the upper four waves' sums go to LDS, the lower four add theirs, then one sum over four
   float* sums = lds + (wave & 3) * ROWS * 64;
   auto at = [&](int k, int t, int e) { return (32 * k + acc_row(half, e)) * 64 + ch + t - ch0; };
@@ -488,20 +483,19 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a,
     for (int i = threadIdx.x; i < a.nb * 64; i += 512) if (ch0 + (i & 63) < a.c) f(i, part + (long long)(i >> 6) * a.c + (i & 63));
   };
   each([&](int i, float* to) { *to = (lds[i] + lds[i + ROWS * 64]) + (lds[i + 2 * ROWS * 64] + lds[i + 3 * ROWS * 64]); });
-  // values that are not finite: whatever their order, the sum is the same infinity or NaN, so the waves may add them to the same words
   if (!__syncthreads_or(odd)) return;
+  // again, lane = channel: every wave goes through all positions and adds those of its buckets (every 8th) to words that are its alone
   for (int i = threadIdx.x; i < ROWS * 64; i += 512) lds[i] = 0.0f;
   __syncthreads();
-  if (ch0 + lane < a.c)
-    for (p = p0 + wave; p < p1; p += 8) {
-      const float f = (float)((const T*)a.d_out)[p * a.c + ch0 + lane];
-      if ((__float_as_uint(f) & 0x7f800000u) != 0x7f800000u) continue;
-      const int q = (int)(p / a.n_k), k = (int)(p - (long long)q * a.n_k);
-      const int b = rb.of(a.pos_q[q], a.pos_k[k], a.seg_q ? a.seg_q[q] : 0, a.seg_q ? a.seg_k[k] : 0);
-      __hip_atomic_fetch_add(lds + b * 64 + lane, f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  const T* column = (const T*)a.d_out + min(ch0 + lane, a.c - 1);
+  for (long long from = p0; from < n; from += apart)
+    for (p = from; p < min(n, from + 128); p++) {
+      const int pos = (int)(p / a.n_k), other = (int)(p - (long long)pos * a.n_k);
+      const int b = rb.of(a.pos_q[pos], a.pos_k[other], a.seg_q ? a.seg_q[pos] : 0, a.seg_q ? a.seg_k[other] : 0);
+      if ((b & 7) == wave) lds_add(lds + b * 64 + lane, (float)column[p * a.c]);
     }
   __syncthreads();
-  each([&](int i, float* to) { *to += lds[i]; });
+  each([&](int i, float* to) { *to = lds[i]; });
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -510,7 +504,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a,
 // [bucket][lane] of its own accumulators (bank = lane whatever the buckets are).  Most lanes' positions are all farther than the outermost
 // edges, which their extremes tell: V elements are then one addition to LDS and no bucket is looked up.
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V, bool WHOLE, int U, int MODE>
+template <typename T, int V, bool WHOLE, int U, int MODE, bool NT>
 __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a) {
   extern __shared__ float acc[];       // [waves][nb][64], then the edges
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -529,7 +523,7 @@ __global__ __launch_bounds__(512) void relpos_heads_bwd_kernel(const RpArgs a) {
     Raw<T, V> next[U];
     auto fetch = [&](int q) {
 #pragma unroll
-      for (int u = 0; u < U; u++) next[u] = sl.load(g + (long long)min(q + u * step, a.n_q - 1) * a.ld);
+      for (int u = 0; u < U; u++) next[u] = sl.template load<NT>(g + (long long)min(q + u * step, a.n_q - 1) * a.ld);
     };
     int q = blockIdx.y * waves + wave;
     if (q < a.n_q) fetch(q);
