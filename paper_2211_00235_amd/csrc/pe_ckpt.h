@@ -1,7 +1,8 @@
 // Activation checkpoints in 8 bits.
 //
-// Groups of 32 consecutive channels of a row share a scale 2^e: the smallest e >= -126 with max|x| <= 127 2^e.  A code is
-// rint(x 2^-e), the value it stands for code 2^e.  A power of two makes every step but that one rounding exact (scaling,
+// Groups of 32 consecutive channels of a row share a scale 2^e: the smallest e >= -126 with max|x| <= 127 2^e, and 121 at most, since
+// 64 2^122 is no number of either type any more (magnitudes above 127 2^121 become that).  A code is
+// rint(x 2^-e) within -127..127, the value it stands for code 2^e.  A power of two makes every step but that one rounding exact (scaling,
 // restoring, and the restored value in bf16: 7 bits of magnitude), so packing what was restored gives the same codes,
 // and the result does not depend on how a division rounds.  The error is at most 2^(e-1), between 1/254 and 1/127 of the group's
 // largest magnitude.  A group that holds an infinity or NaN is restored as NaN throughout: the loss stays visible.
@@ -16,11 +17,11 @@ constexpr int CK_GROUP = 32;
 // largest magnitude's bits (sign cleared) -> the group's scale byte
 PE_DEV uint32_t ck_scale_byte(uint32_t m) {
   const int sb = (int)(m >> 23) - 6 + ((m & 0x7fffffu) > 0x7e0000u ? 1 : 0);     // 64 <= max|x| 2^-e <= 127; above 127/64 of a power of two: the next e
-  return m >= 0x7f800000u ? 255u : (uint32_t)max(sb, 1);
+  return m >= 0x7f800000u ? 255u : (uint32_t)min(max(sb, 1), 248);
 }
-PE_DEV float ck_inverse(uint32_t sb) { return __uint_as_float((254u - sb) << 23); }    // 2^-e, sb 1..249
+PE_DEV float ck_inverse(uint32_t sb) { return __uint_as_float((254u - sb) << 23); }    // 2^-e, sb 1..248
 PE_DEV float ck_scale(uint32_t sb) { return sb == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(sb << 23); }
-PE_DEV int ck_code(float x, float inv) { return (int)rintf(x * inv); }
+PE_DEV int ck_code(float x, float inv) { return (int)rintf(__builtin_amdgcn_fmed3f(x * inv, -127.0f, 127.0f)); }
 
 template <int V> struct Codes;       // V consecutive codes
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
@@ -70,13 +71,14 @@ template <int V, int LG> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>
 // One item = V channels of a row; a row has `per_row` items, a multiple of the LG that share a group (V = 8: 4; V = 1, rows of
 // fewer than 8 channels: 8, one group per row), so item / LG numbers the groups.  A wave takes 64 U consecutive items, all of its
 // loads in flight at once; their scales are 64 U / LG consecutive bytes, stored by as many lanes together.  `flat`: no gaps and
-// whole groups, one long row.  HBM-bound.
+// whole groups, one long row.  HBM-bound.  Workgroups behind the first CK_GRID_X are in further rows of the grid.
+constexpr int CK_GRID_X = 1 << 22;
 template <typename T, int V, bool WHOLE, int U, bool PACK, bool NT>
 __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int8_t* codes, uint8_t* scales, T* y, long long rows,
                                                    int c, int per_row, int flat) {
   constexpr int LG = V == 8 ? 4 : 8;
   const int lane = threadIdx.x & 63;
-  const long long items = rows * per_row, first = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * U);
+  const long long items = rows * per_row, first = (((long long)blockIdx.y * CK_GRID_X + blockIdx.x) * 4 + (threadIdx.x >> 6)) * (64 * U);
   const long long row0 = flat ? 0 : first / per_row;
   const uint32_t rem = flat ? 0 : (uint32_t)(first - row0 * per_row);
   long long at[U], code_at[U];       // element offsets of the row in x or y, and in the codes (flat: of the item)

@@ -36,8 +36,8 @@ def ckpt(x):
         top = np.where(fine, np.abs(np.where(np.isfinite(v), v, 0.0)).max(1), 1.0)
         m, e = np.frexp(top)                                   # top = m 2^e, 0.5 <= m < 1 (e = 0 where top is 0)
         e = np.where(top == 0, -200, np.where(m * 128 <= 127, e - 7, e - 6))
-        e = np.maximum(e, -126)
-        q = np.where(fine[:, None], np.rint(np.where(np.isfinite(v), v, 0.0) / np.exp2(e.astype(np.float64))[:, None]), 0.0)
+        e = np.clip(e, -126, 121)
+        q = np.where(fine[:, None], np.clip(np.rint(np.where(np.isfinite(v), v, 0.0) / np.exp2(e.astype(np.float64))[:, None]), -127, 127), 0.0)
         codes[:, j * GROUP:(j + 1) * GROUP] = q
         scales[:, j] = np.where(fine, e + 127, 255)
         back[:, j * GROUP:(j + 1) * GROUP] = np.where(fine[:, None], q * np.exp2(e.astype(np.float64))[:, None], np.nan)

@@ -245,6 +245,23 @@ def test_ckpt(h, rows, c, dt):
 
 
 @pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("c", [5, 32, 40])
+def test_ckpt_largest_numbers(h, c, dt):
+    """Numbers up to the type's largest stay numbers, off by at most 1/127 of the largest of their group."""
+    top = torch.finfo(dt).max
+    x = torch.tensor([[top], [-top], [top * 0.9961], [top * 0.992], [top / 2]], dtype=torch.float64) * torch.linspace(1.0, -1.0, c, dtype=torch.float64)
+    t = x.to(dt).cuda()
+    kept, y, again = bytes_(pe.ckpt_bytes(5, c)), torch.empty_like(t), bytes_(pe.ckpt_bytes(5, c))
+    pe.ckpt_pack(h, t, kept)
+    pe.ckpt_unpack(h, kept, y)
+    T, Y = f64(t), f64(y)
+    assert np.isfinite(Y).all() and np.array_equal(Y, ref.ckpt(T)[2])
+    assert (np.abs(Y - T)[:, :32] <= np.abs(T[:, :32]).max(1, keepdims=True) / 127).all()
+    pe.ckpt_pack(h, y, again)
+    assert torch.equal(again[:5 * c], kept[:5 * c])
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
 @pytest.mark.parametrize("c, ld, off", [(64, 72, 0), (64, 65, 0), (64, 80, 1), (40, 48, 8), (23, 40, 3), (130, 132, 4)])
 def test_ckpt_strided_rows(h, c, ld, off, dt):
     rng = np.random.default_rng(ld)
