@@ -366,7 +366,7 @@ int pe_ckpt_unpack(pe_handle* h, long long rows, int c, int dtype, const void* c
  * The distances clipped to +-32 of a protein's residues are edges -31, -30 .. 32.  One new position against a long sequence is n_q = 1. */
 enum { PE_RELPOS_PAIR = 0, PE_RELPOS_HEADS = 1 };
 typedef struct pe_relpos {
-  int n_q, n_k;          /* 0 .. 2^27                                                  */
+  int n_q, n_k;          /* 0 .. 2^24                                                  */
   int c;                 /* channels or heads, 1 .. 1024; n_q * n_k * c up to 10^12    */
   int n_edges;           /* 0 .. 254                                                   */
   int segments;          /* 0: none, 1: seg_q and seg_k are given                      */

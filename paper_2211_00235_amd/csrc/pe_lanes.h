@@ -56,14 +56,12 @@ template <int L> PE_DEV uint32_t lanes_umax(uint32_t v) {
 // element's alignment only (global accesses of 16 bytes may start at any byte).
 template <typename T, int V> struct Raw;
 template <> struct Raw<bf16, 8> { bf16x8 v; PE_DEV float get(int i) const { return (float)v[i]; } PE_DEV void set(int i, float f) { v[i] = (bf16)f; } };
-template <> struct Raw<bf16, 2> { bf16x2 v; PE_DEV float get(int i) const { return (float)v[i]; } PE_DEV void set(int i, float f) { v[i] = (bf16)f; } };
 template <> struct Raw<bf16, 1> { bf16 v; PE_DEV float get(int) const { return (float)v; } PE_DEV void set(int, float f) { v = (bf16)f; } };
 template <> struct Raw<float, 8> {
   f32x4 v[2];
   PE_DEV float get(int i) const { return v[i >> 2][i & 3]; }
   PE_DEV void set(int i, float f) { v[i >> 2][i & 3] = f; }
 };
-template <> struct Raw<float, 2> { f32x2 v; PE_DEV float get(int i) const { return v[i]; } PE_DEV void set(int i, float f) { v[i] = f; } };
 template <> struct Raw<float, 1> { float v; PE_DEV float get(int) const { return v; } PE_DEV void set(int, float f) { v = f; } };
 // NT: a non-temporal load, for tensors that are read once and much larger than what the caches keep: lines that such a stream allocates push
 // out what the kernels before have written, whose way to memory then stands in the stream's.
@@ -133,9 +131,6 @@ template <int V> PE_DEV void load_f32(const float* p, float (&v)[V]) {
     const f32x4_any a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
 #pragma unroll
     for (int i = 0; i < 4; i++) { v[i] = a[i]; v[4 + i] = b[i]; }
-  } else if constexpr (V == 2) {
-    const f32x2_any a = *reinterpret_cast<const f32x2_any*>(p);
-    v[0] = a[0]; v[1] = a[1];
   } else {
     v[0] = *p;
   }

@@ -203,7 +203,7 @@ void columns_sum(OpCall& op, const char* label, const float* part, long long n_p
 // ---------------------------------------------------------------------------------------------------------------------
 int rp_buckets(const pe_relpos& p) { return p.n_edges + 1 + (p.segments ? 1 : 0); }
 const char* rp_why(const pe_relpos& p) {
-  if (p.n_q < 0 || p.n_k < 0 || p.n_q > (1 << 27) || p.n_k > (1 << 27)) return "relative positions: n_q and n_k in [0, 2^27]";
+  if (p.n_q < 0 || p.n_k < 0 || p.n_q > (1 << 24) || p.n_k > (1 << 24)) return "relative positions: n_q and n_k in [0, 2^24]";
   if (p.c < 1 || p.c > 1024) return "relative positions: c in [1, 1024]";
   if ((double)p.n_q * p.n_k * p.c > 1e12) return "relative positions: n_q * n_k * c up to 10^12";
   if (p.n_edges < 0 || p.n_edges > RP_MAX_EDGES) return "relative positions: n_edges in [0, 254]";
@@ -279,14 +279,13 @@ template <typename F> void rp_dispatch(int mode, bool few, F&& f) {
 template <typename F> void rp_dispatch_few(int mode, F&& f) {
   if (mode == RP_DENSE) f(std::integral_constant<int, RP_DENSE>{}); else f(std::integral_constant<int, RP_SEARCH>{});
 }
-// PAIR, channels per access: 8 (16 bytes) or 1
-template <typename T, int V> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
+template <typename T, int V, bool WHOLE> void rp_pair_fwd(hipStream_t st, const RpArgs& a) {
   constexpr int U = V == 8 ? 4 : 8;
-  const int vecs = a.c / V;
-  const int tile = std::max(1, 256 * U / vecs);          // vecs <= 1024 <= 256 U (c <= 1024): at least one position
+  const int vecs = (a.c + V - 1) / V;
+  const int tile = 256 * U / vecs;                       // vecs <= 128 (c <= 1024): several positions
   const unsigned magic = vecs == 1 ? 0u : (unsigned)(((1ull << 32) + vecs - 1) / vecs);     // exact for vectors up to 2^11
   const unsigned gx = (unsigned)((a.n_k + tile - 1) / tile), gy = (unsigned)std::min(a.n_q, 65535), gz = (unsigned)((a.n_q + 65534) / 65535);
-  rp_dispatch_few(a.mode, [&](auto m) { hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, U, m.value>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile, magic); });
+  rp_dispatch_few(a.mode, [&](auto m) { hipLaunchKernelGGL((relpos_pair_fwd_kernel<T, V, WHOLE, U, m.value>), dim3(gx, gy, gz), dim3(256), 0, st, a, tile, vecs, magic); });
 }
 template <typename T, int V, bool WHOLE> void rp_heads_fwd(hipStream_t st, const RpArgs& a) {
   // heads per workgroup: what 32 KB of LDS hold, and few enough that the chip is filled
@@ -334,15 +333,16 @@ template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int d
     });
   });
 }
-// The matrix unit's kernel: up to 128 buckets, rows without gaps, more than 16 channels, a batch of positions at least
-bool rp_pair_mm(const RpArgs& a) { return a.nb <= 128 && a.c > 16 && a.ld == (long long)a.n_k * a.c && (long long)a.n_q * a.n_k >= 16; }
+// The matrix unit's kernel: rows without gaps, more than 16 channels, a batch of positions at least
+bool rp_pair_mm(const RpArgs& a) { return a.c > 16 && a.ld == (long long)a.n_k * a.c && (long long)a.n_q * a.n_k >= 16; }
 template <typename T, int NB> void rp_pair_bwd_mm(hipStream_t st, int device, const RpArgs& a, long long groups) {
   rp_dispatch_few(a.mode, [&](auto m) {
     stream_dispatch((double)a.n_q * a.n_k * a.c * sizeof(T), [&](auto nt) {
       static std::atomic<unsigned long long> done{0};
       allow_lds(&relpos_pair_bwd_mm_kernel<T, NB, m.value, nt.value>, device, done);
       const size_t lds = (size_t)4 * NB * 32 * 64 * 4 + 512 + 4 * rp_lds_words(m.value);
-      hipLaunchKernelGGL((relpos_pair_bwd_mm_kernel<T, NB, m.value, nt.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64)), dim3(512), lds, st, a);
+      hipLaunchKernelGGL((relpos_pair_bwd_mm_kernel<T, NB, m.value, nt.value>), dim3((unsigned)groups, (unsigned)((a.c + 63) / 64), (unsigned)((a.nb + 32 * NB - 1) / (32 * NB))),
+                         dim3(512), lds, st, a);
     });
   });
 }
@@ -502,9 +502,9 @@ int pe_relpos_fwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
         using T = decltype(t);
         // little to write: a position per lane, so that eight times the workgroups share it (1 x 8191 x 8: 3.7 us, by vectors 7.1)
         if (!pair && n < (1 << 19)) rp_heads_fwd<T, 1, true>(op.st, a);
-        else if (!pair) width_dispatch(p->n_k, whole, [&](auto v, auto w) { rp_heads_fwd<T, v.value, w.value>(op.st, a); });
-        else if (whole) rp_pair_fwd<T, 8>(op.st, a);
-        else rp_pair_fwd<T, 1>(op.st, a);
+        else width_dispatch(pair ? p->c : p->n_k, whole, [&](auto v, auto w) {
+          if (pair) rp_pair_fwd<T, v.value, w.value>(op.st, a); else rp_heads_fwd<T, v.value, w.value>(op.st, a);
+        });
       });
     });
     return op.err;
@@ -537,7 +537,7 @@ int pe_relpos_bwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
       const bool whole = Whole(p->n_k, e).take(d_out, a.ld, 2).ok;
       groups = pair ? rp_pair_groups(*p) : rp_heads_groups(*p);
       const double n = (double)p->n_q * p->n_k * p->c;
-      op.launch("relpos bwd", pair ? "relpos_pair_bwd_kernel" : "relpos_heads_bwd_kernel", n, n * e, [&] {
+      op.launch("relpos bwd", pair ? rp_pair_mm(a) ? "relpos_pair_bwd_mm_kernel" : "relpos_pair_bwd_kernel" : "relpos_heads_bwd_kernel", n, n * e, [&] {
         type_dispatch(p->dtype, [&](auto t) {
           using T = decltype(t);
           if (pair) rp_pair_bwd_run<T>(op.st, h->device, a, groups);

@@ -102,14 +102,14 @@ template <int V> struct RpLane {
 // PAIR, forward: a workgroup has one q and tile_k positions k.  A lane has V channels of U positions; the positions' numbers and
 // `add` are requested together, then the U table rows, so two round trips to memory lie one behind the other.  Lanes find their
 // buckets each for itself: with buckets passed through LDS two barriers joined the chain (16.8 MB written and read: 21 us).
-// vec_magic: ceil(2^32 / vectors per position), 0 for 1
+// vecs: vectors per position; vec_magic: ceil(2^32 / vecs), 0 for 1
 // ---------------------------------------------------------------------------------------------------------------------
-template <typename T, int V, int U, int MODE>
-__global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, int tile_k, uint32_t vec_magic) {
+template <typename T, int V, bool WHOLE, int U, int MODE>
+__global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, int tile_k, int vecs, uint32_t vec_magic) {
   __shared__ int edges[rp_lds_words(MODE)];
   const int q = blockIdx.y + blockIdx.z * 65535, k0 = blockIdx.x * tile_k;
   if (q >= a.n_q) return;
-  const int nk = min(tile_k, a.n_k - k0), vecs = a.c / V, total = nk * vecs;
+  const int nk = min(tile_k, a.n_k - k0), total = nk * vecs;
   const long long base = (long long)q * a.ld + (long long)k0 * a.c;
   const T* add = (const T*)a.add;
   T* out = (T*)a.out;
@@ -122,9 +122,10 @@ __global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, in
     pk[u] = a.pos_k[k0 + k[u]];
     sk[u] = a.seg_q ? a.seg_k[k0 + k[u]] : 0;
   }
+  auto slot = [&](int u) { return Slot<V, WHOLE>(e[u] - k[u] * vecs, a.c); };
   if (add)
 #pragma unroll
-    for (int u = 0; u < U; u++) ad[u] = raw_load<T, V>(add + base + (long long)e[u] * V);
+    for (int u = 0; u < U; u++) ad[u] = slot(u).load(add + base + k[u] * a.c);
   const int pq = a.pos_q[q], sq = a.seg_q ? a.seg_q[q] : 0;
   if constexpr (MODE != RP_DENSE) {
     RpBuckets<MODE>::fill(edges, a);
@@ -133,13 +134,13 @@ __global__ __launch_bounds__(256) void relpos_pair_fwd_kernel(const RpArgs a, in
   const RpBuckets<MODE> rb(edges, a);
   float t[U][V];
 #pragma unroll
-  for (int u = 0; u < U; u++) load_f32<V>(a.table + (long long)rb.of(pq, pk[u], sq, sk[u]) * a.c + (e[u] - k[u] * vecs) * V, t[u]);
+  for (int u = 0; u < U; u++) load_f32<V>(a.table + (long long)rb.of(pq, pk[u], sq, sk[u]) * a.c + slot(u).at, t[u]);
 #pragma unroll
   for (int u = 0; u < U; u++) {
     Raw<T, V> o;
 #pragma unroll
     for (int i = 0; i < V; i++) o.set(i, add ? ad[u].get(i) + t[u][i] : t[u][i]);
-    if ((int)threadIdx.x + 256 * u < total) raw_store<T, V>(out + base + (long long)e[u] * V, o);
+    if ((int)threadIdx.x + 256 * u < total) slot(u).store(out + base + k[u] * a.c, o);
   }
 }
 
@@ -204,8 +205,9 @@ PE_DEV void lds_add(float* p, float v) { *p += v; }
 // accumulators.  Neighbouring positions of the same bucket (all that are farther than the outermost edges) are added in a register
 // first, which the whole wave decides together where it has one position at a time.  S positions share a wave where c <= 32.
 // blockIdx.y: slab of 64 channels (S = 1).  NEAR: offsets of d_out in bytes fit 32 bits, which
-// halves the instructions of a load.  The loads of a batch are in flight per wave; lanes behind the last channel or position load a valid one,
-// since a load under a condition is waited for by itself (2 bytes per lane and 126 us at 384 x 384 x 128).
+// halves the instructions of a load.  A batch of loads is in flight per wave; lanes behind the last channel or position load a valid one,
+// since a load under a condition is waited for by itself.  For what the kernel below does not take: rows with gaps (384 x 384 x 128 with the
+// sums 21 us, the kernel below 18 without gaps) and up to 16 channels (384 x 384 x 16: 11.5).
 // ---------------------------------------------------------------------------------------------------------------------
 template <typename T, int S, int U, int MODE, bool NEAR>
 __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a) {
@@ -320,7 +322,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_kernel(const RpArgs a) {
 // PAIR, backward, on the matrix unit: d_table[32 buckets][32 channels] += H D with H[bucket][position] = 1 where the position is in the
 // bucket, 0 elsewhere, and D = d_out[position][channel], 16 positions at a time.  The products are exact, sums fp32, and buckets in any
 // order cost the same; blocks of 32 buckets without a position among the 16 are left out.  A wave has 64 channels, two neighbouring ones
-// per lane (a load of the wave is two positions' 128 or 256 bytes; with one channel per lane the same products took twice the time),
+// per lane (a load of the wave is two positions' 128 or 256 bytes),
 // and every 8th batch of 16 positions; its sums stay in registers.
 // 0 times infinity is NaN: a value that is not finite makes sums of other buckets NaN too, and a workgroup that finds such a sum in the
 // end forms all of its sums again without products.
@@ -363,7 +365,8 @@ template <> struct RpPairs<float> {
   }
 };
 
-// NB: blocks of 32 buckets.  LDS: [4][NB * 32][64] sums, 64 bytes of buckets per wave, the edges.  c >= 2, n_q n_k >= 16.
+// NB: blocks of 32 buckets, from 32 NB blockIdx.z on (what a wave's registers hold: more than 128 buckets are two workgroups' that both read
+// d_out: 201 buckets over 384 x 384 x 128 with the sums 40 us, by the kernel above 66).  LDS: [4][NB * 32][64] sums, 64 bytes of buckets per wave, the edges.  c >= 2, n_q n_k >= 16.
 template <typename T, int NB, int MODE, bool NT>
 __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a) {
   extern __shared__ float lds[];
@@ -371,13 +374,13 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
   uint8_t* bytes = reinterpret_cast<uint8_t*>(lds + 4 * ROWS * 64) + wave * 64;
   int* edges = reinterpret_cast<int*>(lds + 4 * ROWS * 64 + 128);
+  const int b0 = ROWS * blockIdx.z, nb = min(ROWS, a.nb - b0);
   const int ch0 = blockIdx.y * 64, ch = min(ch0 + 2 * col, a.c - 2);           // lanes behind the last channels load those two
   const long long n = (long long)a.n_q * a.n_k;
   const int* seg_q = a.seg_q ? a.seg_q : a.pos_q;            // without segments: loaded and not used
   const int* seg_k = a.seg_q ? a.seg_k : a.pos_k;
-  // The workgroups take 128 positions (16 per wave) in turn, so that all of them read neighbouring memory: with a range of its own for
-  // each, all moved through the memory's channels together (1024 x 1024 x 128 MM_RANGE us).  A wave's round is four of its batches; lane l has
-  // the place of position l % 16 of batch l / 16, and steps from round to round without a division.
+  // The workgroups take 128 positions (16 per wave) in turn.  A wave's round is four of its batches; lane l has the place of position
+  // l % 16 of batch l / 16, and steps from round to round without a division.
   const int apart = 128 * gridDim.x, step = 4 * apart;
   const long long p0 = 128LL * blockIdx.x;
   long long p = p0 + 16 * wave;
@@ -426,7 +429,7 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a)
       for (int e = 0; e < 16; e++) acc[k][t][e] = 0.0f;
   for (; p < n; p += step) {
     const bool in = p + mine_at < n;
-    const int b = rb.of(now.pq, now.pk, a.seg_q ? now.sq : 0, a.seg_q ? now.sk : 0);
+    const int b = rb.of(now.pq, now.pk, a.seg_q ? now.sq : 0, a.seg_q ? now.sk : 0) - b0;      // as a byte outside of 0..127: no row here
     const long long behind = p + apart * (lane >> 4) + 16 - n;
     const int shift = behind > 0 ? (int)min(behind, 16LL) : 0;                 // places that the batch was moved down by
     bytes[lane] = 255;                                       // no row
@@ -478,9 +481,9 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a)
             }
     __syncthreads();
   }
-  float* part = a.part + (long long)blockIdx.x * a.nb * a.c + ch0;
+  float* part = a.part + ((long long)blockIdx.x * a.nb + b0) * a.c + ch0;
   auto each = [&](auto&& f) {
-    for (int i = threadIdx.x; i < a.nb * 64; i += 512) if (ch0 + (i & 63) < a.c) f(i, part + (long long)(i >> 6) * a.c + (i & 63));
+    for (int i = threadIdx.x; i < nb * 64; i += 512) if (ch0 + (i & 63) < a.c) f(i, part + (long long)(i >> 6) * a.c + (i & 63));
   };
   each([&](int i, float* to) { *to = (lds[i] + lds[i + ROWS * 64]) + (lds[i + 2 * ROWS * 64] + lds[i + 3 * ROWS * 64]); });
   if (!__syncthreads_or(odd)) return;
@@ -491,8 +494,8 @@ __global__ __launch_bounds__(512) void relpos_pair_bwd_mm_kernel(const RpArgs a)
   for (long long from = p0; from < n; from += apart)
     for (p = from; p < min(n, from + 128); p++) {
       const int pos = (int)(p / a.n_k), other = (int)(p - (long long)pos * a.n_k);
-      const int b = rb.of(a.pos_q[pos], a.pos_k[other], a.seg_q ? a.seg_q[pos] : 0, a.seg_q ? a.seg_k[other] : 0);
-      if ((b & 7) == wave) lds_add(lds + b * 64 + lane, (float)column[p * a.c]);
+      const int b = rb.of(a.pos_q[pos], a.pos_k[other], a.seg_q ? a.seg_q[pos] : 0, a.seg_q ? a.seg_k[other] : 0) - b0;
+      if (b >= 0 && b < nb && (b & 7) == wave) lds_add(lds + b * 64 + lane, (float)column[p * a.c]);
     }
   __syncthreads();
   each([&](int i, float* to) { *to = lds[i]; });

@@ -78,9 +78,9 @@ int main() {
   CK(PE_OK, a.rows = 0; a.t = a.k = nullptr);
   // relative positions
   RP(PE_ERR_ARG, );
-  RP(PE_ERR_DIMS, a.p.n_q = -1); RP(PE_ERR_DIMS, a.p.n_k = (1 << 27) + 1); RP(PE_ERR_DIMS, a.p.c = 0); RP(PE_ERR_DIMS, a.p.c = 1025); RP(PE_ERR_DIMS, a.p.n_edges = -1);
+  RP(PE_ERR_DIMS, a.p.n_q = -1); RP(PE_ERR_DIMS, a.p.n_k = (1 << 24) + 1); RP(PE_ERR_DIMS, a.p.c = 0); RP(PE_ERR_DIMS, a.p.c = 1025); RP(PE_ERR_DIMS, a.p.n_edges = -1);
   RP(PE_ERR_DIMS, a.p.n_edges = 255); RP(PE_ERR_DIMS, a.p.segments = 2); RP(PE_ERR_DIMS, a.p.layout = 2); RP(PE_ERR_DIMS, a.p.dtype = PE_CKPT); RP(PE_ERR_DIMS, a.p.ld = -1);
-  RP(PE_ERR_DIMS, a.p.n_q = a.p.n_k = 1 << 27);
+  RP(PE_ERR_DIMS, a.p.n_q = a.p.n_k = 1 << 24);
   RP(PE_ERR_ARG, a.p.ld = 12 * 8 - 1); RP(PE_ERR_ARG, a.p.layout = PE_RELPOS_HEADS; a.p.ld = 11);
   static const int same[3] = {-1, -1, 5}, down[3] = {0, -1, 5}, least[3] = {-2147483647 - 1, 0, 5};
   RP(PE_ERR_ARG, a.edges = same); RP(PE_ERR_ARG, a.edges = down); RP(PE_ERR_ARG, a.edges = least);

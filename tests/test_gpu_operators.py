@@ -328,6 +328,25 @@ def test_relpos(h, layout, dt, n_q, n_k, c, edges, segs):
     inside(dt_, ref.relpos_bwd(b, f64(d), nb, layout), (64 + n_q * n_k / 4) * U * ref.relpos_bwd(b, np.abs(f64(d)), nb, layout))
 
 
+@pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("n_q, n_k, c, edges, off", [(20, 30, 65, CLIP, 0), (19, 33, 129, LOG, 1), (31, 17, 191, CLIP, 3), (23, 40, 64, CLIP, 1), (9, 50, 11, LOG, 5)])
+def test_relpos_pair_odd_channels_and_alignment(h, n_q, n_k, c, edges, off, dt):
+    """Positions whose channels are no whole 16-byte pieces, or start between two; what lies around them stays."""
+    rng = np.random.default_rng(n_q + c)
+    pq, pk, ed, _, _, table, b, nb = rp_inputs(rng, n_q, n_k, edges, False, c)
+    n = n_q * n_k * c
+    buf = rand(rng, (off + n + 40,), dt)
+    was, view = buf.clone(), buf[off:off + n].view(n_q, n_k, c)
+    want = ref.relpos(b, f64(table), f64(view), "pair")
+    pe.relpos_fwd(h, pq, pk, ed, table, view, add=view, layout="pair")
+    inside(view, want, HALF[dt] * np.abs(want) * (1 + 1e-6) + U * np.abs(want))
+    assert torch.equal(buf[:off], was[:off]) and torch.equal(buf[off + n:], was[off + n:])
+    view.copy_(torch.from_numpy(rng.integers(-8, 9, size=(n_q, n_k, c))))                  # whole numbers: exact sums
+    d = torch.full((nb, c), 5.0, device="cuda")
+    pe.relpos_bwd(h, pq, pk, ed, view, d, bytes_(pe.relpos_workspace_bytes(n_q, n_k, c, nb, "pair")), layout="pair")
+    assert np.array_equal(f64(d), ref.relpos_bwd(b, f64(view), nb, "pair"))
+
+
 @pytest.mark.parametrize("layout", ["pair", "heads"])
 @pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
 @pytest.mark.parametrize("n_q, n_k, c, edges", [(40, 64, 64, CLIP), (33, 50, 33, LOG), (21, 47, 20, CLIP), (40, 64, 8, CLIP), (17, 90, 48, MANY)])
