@@ -350,8 +350,9 @@ int pe_layernorm_bwd(pe_handle* h, long long rows, int c, int dtype, int x_type,
 
 /* Activation checkpoint: [rows][c] in 8 bits, c in [1, 2^20].  Groups of 32 consecutive channels of a row (the last one may
  * be shorter) share a scale 2^e, the smallest e >= -126 with max|x| <= 127 * 2^e (121 at most); a code is x / 2^e rounded to
- * the nearest integer, ties to even, and 127 at most in magnitude.  What is restored is code * 2^e, exactly, in either type; a group that holds an infinity or NaN
- * is restored as NaN.  The error is at most 1/127 of the group's largest magnitude (or 2^-127).
+ * the nearest integer, ties to even, and 127 at most in magnitude.  What is restored is code * 2^e, exactly, in either type;
+ * a group that holds an infinity or NaN is restored as NaN.  The error is at most 1/127 of the group's largest magnitude (or
+ * 2^-127).
  * Layout: codes int8 [rows][c]; from the next multiple of 256 bytes on one byte e + 127 per group, [rows][ceil(c / 32)], 255
  * for a group that was not finite.                                                                       */
 size_t pe_ckpt_bytes(long long rows, int c);

@@ -6,7 +6,7 @@
 //
 // HBM-bound: 8 vector operations per element forward, 15 backward, against 4 to 8 bytes.  A row lies in the registers of L
 // lanes (NV vectors of V elements each), so that it is read once: L = 4..64 lanes, several rows per wave, up to 1024 channels,
-// whole workgroups above.  Channel counts and alignments without 16-byte accesses take the same kernels with WHOLE = false; rows of fewer
+// whole workgroups above.  Other channel counts and alignments than whole, aligned 16-byte pieces take the same kernels with WHOLE = false; rows of fewer
 // than 8 channels have a lane per channel.  Statistics and sums are fp32; a result is rounded once, to the storage type.  A lane keeps its columns'
 // d_gain and d_offset in registers over all of its rows; workgroups write one fp32 partial each, and columns_sum_kernel adds
 // them in a fixed order.
