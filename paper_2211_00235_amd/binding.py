@@ -410,8 +410,8 @@ def _relpos(h, pos_q, pos_k, edges, t, seg_q, seg_k, layout, what):
         raise PEError("%s: shape differs from the positions'" % what)
     ld = 0
     if not t.is_contiguous():
-        ok = st[2] == 1 and (st[1] == c if pair else st[0] == n_q * st[1])
-        ld = st[0] if pair else st[1]
+        ld = st[0] if pair or n_q == 1 else st[1]            # the stride of an axis of one element says nothing
+        ok = (st[2] == 1 or s[2] == 1) and ((st[1] == c or n_k == 1) if pair else (st[0] == n_q * ld or c == 1))
         if not ok or ld < (n_k * c if pair else n_k):
             raise PEError("%s: gaps are allowed between rows q only" % what)
     p = _Relpos(n_q, n_k, c, edges.numel(), 0 if seg_q is None else 1, _LAYOUTS[layout], d, ld)
@@ -425,7 +425,7 @@ def relpos_fwd(h, pos_q, pos_k, edges, table, out, seg_q=None, seg_k=None, add=N
     p, ptr, n = _relpos(h, pos_q, pos_k, edges, out, seg_q, seg_k, layout, "out")
     if add is not None:
         _on(h, add, "add")
-        if add.dtype != out.dtype or add.shape != out.shape or add.stride() != out.stride():
+        if add.dtype != out.dtype or add.shape != out.shape or (add.stride() != out.stride() and not (add.is_contiguous() and out.is_contiguous())):
             raise PEError("add: laid out as out is wanted")
     _op(h, lib().pe_relpos_fwd(h._h, C.byref(p), *ptr, _vec(h, table, n, "table"), None if add is None else add.data_ptr(),
                                out.data_ptr(), _s(stream)), "pe_relpos_fwd")

@@ -389,6 +389,37 @@ def test_relpos_rows_with_gaps(h, layout, gap):
     assert torch.equal(buf, was)
 
 
+def test_relpos_axes_of_one_element(h):
+    """One new position's rows in a longer sequence's bias and pair representation; what lies around them stays."""
+    rng = np.random.default_rng(8)
+    n, c, at = 72, 16, 29
+    pos = torch.arange(n, device="cuda", dtype=torch.int32)
+    ed, table = torch.tensor(LOG, dtype=torch.int32), vec(rng, (len(LOG) + 1) * c).view(-1, c)
+    b = ref.buckets(np.array([at]), np.arange(n), LOG)
+    bias, pair = rand(rng, (c, n, n), torch.float32), rand(rng, (n, n, c), torch.float32)
+    for layout, whole, view in (("heads", bias, bias[:, at:at + 1]), ("heads", bias, bias[3:4, at:at + 1]), ("pair", pair, pair[at:at + 1]), ("pair", pair, pair[at:at + 1, :, 5:6])):
+        cc = view.shape[0] if layout == "heads" else view.shape[2]
+        if layout == "pair" and cc == 1:                     # channels of one position each, apart
+            with pytest.raises(pe.PEError, match="gaps"):
+                pe.relpos_fwd(h, pos[at:at + 1], pos, ed, table[:, :1].contiguous(), view, layout=layout)
+            continue
+        tab, was, old = table[:, :cc].contiguous(), whole.clone(), view.clone()
+        pe.relpos_fwd(h, pos[at:at + 1], pos, ed, tab, view, layout=layout)
+        assert np.array_equal(f64(view), ref.relpos(b, f64(tab), None, layout))
+        d = torch.empty(len(LOG) + 1, cc, device="cuda")
+        view.copy_(torch.from_numpy(rng.integers(-8, 9, size=tuple(view.shape))))
+        pe.relpos_bwd(h, pos[at:at + 1], pos, ed, view, d, bytes_(pe.relpos_workspace_bytes(1, n, cc, len(LOG) + 1, layout)), layout=layout)
+        assert np.array_equal(f64(d), ref.relpos_bwd(b, f64(view), len(LOG) + 1, layout))
+        view.copy_(old)
+        assert torch.equal(whole, was)
+    column = pair[:, at:at + 1]                              # n_k = 1
+    was, want = pair.clone(), ref.relpos(ref.buckets(np.arange(n), np.array([at]), LOG), f64(table), f64(column), "pair")
+    pe.relpos_fwd(h, pos, pos[at:at + 1], ed, table, column, add=column)
+    inside(column, want, HALF[torch.float32] * np.abs(want) * (1 + 1e-6) + U * np.abs(want))
+    pair[:, at] = was[:, at]
+    assert torch.equal(pair, was)
+
+
 def test_relpos_extreme_positions(h):
     """Differences beyond 32 bits fall into the outermost buckets."""
     big = 2147483647
