@@ -71,7 +71,7 @@ template <int V, int LG> PE_DEV uint32_t ck_encode(const float (&x)[V], Codes<V>
 // One item = V channels of a row; a row has `per_row` items, a multiple of the LG that share a group (V = 8: 4; V = 1, rows of
 // fewer than 8 channels: 8, one group per row), so item / LG numbers the groups.  A wave takes 64 U consecutive items, all of its
 // loads in flight at once; their scales are 64 U / LG consecutive bytes, stored by as many lanes together.  `flat`: no gaps and
-// whole groups, one long row.  HBM-bound.  Workgroups behind the first CK_GRID_X are in further rows of the grid.
+// whole groups; whole vectors then need no rows, it is one long row.  HBM-bound.  Workgroups behind the first CK_GRID_X are in further rows of the grid.
 constexpr int CK_GRID_X = 1 << 22;
 template <typename T, int V, bool WHOLE, int U, bool PACK, bool NT>
 __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int8_t* codes, uint8_t* scales, T* y, long long rows,
@@ -79,8 +79,9 @@ __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int
   constexpr int LG = V == 8 ? 4 : 8;
   const int lane = threadIdx.x & 63;
   const long long items = rows * per_row, first = (((long long)blockIdx.y * CK_GRID_X + blockIdx.x) * 4 + (threadIdx.x >> 6)) * (64 * U);
-  const long long row0 = flat ? 0 : first / per_row;
-  const uint32_t rem = flat ? 0 : (uint32_t)(first - row0 * per_row);
+  const bool line = WHOLE && flat;
+  const long long row0 = line ? 0 : first / per_row;
+  const uint32_t rem = line ? 0 : (uint32_t)(first - row0 * per_row);
   long long at[U], code_at[U];       // element offsets of the row in x or y, and in the codes (flat: of the item)
   int vec[U];
   bool in[U];
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(256) void ckpt_kernel(const T* x, long long ld, int
 #pragma unroll
   for (int u = 0; u < U; u++) {
     const long long item = first + 64 * u + lane;
-    if (WHOLE && flat) {
+    if (line) {
       in[u] = item < items;
       vec[u] = 0;
       at[u] = code_at[u] = item * V;
