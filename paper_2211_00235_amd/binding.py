@@ -275,6 +275,11 @@ def stack_fwd_bwd(h, n_extra, extra, n_main, main, extra_msa_in, msa_in, pair_in
 _DTYPES = {}      # by torch type, filled as types come
 
 
+def _int32(*sizes):
+    """Whether sizes fit the C int that they are passed as (ctypes keeps the low 32 bits, which may be a size in range)."""
+    return all(-2 ** 31 <= n < 2 ** 31 for n in sizes)
+
+
 def _dtype(t):
     d = _DTYPES.get(t.dtype)
     if d is None:
@@ -298,6 +303,8 @@ def _rows(h, t, what, like=None):
     if (d != PE_F32 and d != PE_BF16) or not shape:
         raise PEError("%s: a float32 or bfloat16 tensor [..., c] is wanted" % what)
     c = shape[-1]
+    if c >> 31:
+        raise PEError("%s: %d channels are more than an operator takes" % (what, c))
     if t.is_contiguous():
         rows, ld = (t.numel() // c if c else 0), c
     elif len(shape) == 2 and (c == 1 or t.stride(1) == 1):
@@ -347,7 +354,7 @@ def layernorm_fwd(h, x, gain, offset, y, eps=1e-5, add=None, stats=None, ckpt=No
 
 
 def layernorm_workspace_bytes(rows, c):
-    return int(lib().pe_layernorm_workspace_bytes(rows, c))
+    return int(lib().pe_layernorm_workspace_bytes(rows, c)) if _int32(c) else 0
 
 
 def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=None, accumulate=False, stream=None):
@@ -371,7 +378,7 @@ def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=No
 
 
 def ckpt_bytes(rows, c):
-    return int(lib().pe_ckpt_bytes(rows, c))
+    return int(lib().pe_ckpt_bytes(rows, c)) if _int32(c) else 0
 
 
 def ckpt_pack(h, x, ckpt, stream=None):
@@ -408,6 +415,8 @@ def _relpos(h, pos_q, pos_k, edges, t, seg_q, seg_k, layout, what):
     c = s[2] if pair else s[0]
     if tuple(s) != ((n_q, n_k, c) if pair else (c, n_q, n_k)):
         raise PEError("%s: shape differs from the positions'" % what)
+    if (n_q | n_k | c | edges.numel()) >> 31:
+        raise PEError("%s: n_q and n_k up to 2^24, c up to 1024 and 254 edges are wanted" % what)
     ld = 0
     if not t.is_contiguous():
         ld = st[0] if pair or n_q == 1 else st[1]            # the stride of an axis of one element says nothing
@@ -434,6 +443,8 @@ def relpos_fwd(h, pos_q, pos_k, edges, table, out, seg_q=None, seg_k=None, add=N
 def relpos_workspace_bytes(n_q, n_k, c, buckets, layout="pair"):
     """Bytes for relpos_bwd; buckets: rows of the table."""
     segments = int(buckets > 1)
+    if not _int32(n_q, n_k, c, buckets):
+        return 0
     p = _Relpos(n_q, n_k, c, buckets - 1 - segments, segments, _LAYOUTS[layout], PE_F32, 0)
     return int(lib().pe_relpos_workspace_bytes(C.byref(p)))
 
