@@ -1,6 +1,8 @@
-"""ctypes binding of include/pe.h.  Argument marshalling only."""
+"""ctypes binding of include/pe.h.  Argument marshalling only.  A call whose stream is left out runs on the stream that is current in
+torch on the handle's device; 0 is the default stream."""
 import ctypes as C
 import os
+import sys
 
 PE_F32, PE_BF16, PE_CKPT = 0, 1, 2
 PE_RELPOS_PAIR, PE_RELPOS_HEADS = 0, 1
@@ -215,10 +217,28 @@ def _p(t):
     return C.c_void_p(t.data_ptr())
 
 
-def _s(stream):
-    if stream is None:
+_raw_stream = None      # torch's function device -> pointer of the current stream, once torch uses the GPU
+
+
+def _find_raw_stream():
+    global _raw_stream
+    torch = sys.modules.get("torch")
+    if torch is None or not torch.cuda.is_initialized():
         return None
-    return C.c_void_p(getattr(stream, "cuda_stream", stream))
+    # 0.1 us; by the public call 1.1, a sixth of a small operator's call
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw_stream
+
+
+def _current_stream(device):
+    """The stream that is current in torch on a device (0: the default stream, also where torch does not use the GPU)."""
+    raw = _raw_stream or _find_raw_stream()
+    return raw(device) if raw is not None else 0
+
+
+def _s(h, stream):
+    """hipStream_t of a stream argument: a torch stream, a pointer (0: the default stream), or None: torch's current stream."""
+    return _current_stream(h.device) if stream is None else getattr(stream, "cuda_stream", stream)
 
 
 def _raise(h, rc, what, dims=None):
@@ -231,7 +251,7 @@ def block_fwd(h, dims, msa_in, pair_in, msa_mask, pair_mask, params, msa_out, pa
               stream_msa=None, stream_pair=None):
     rc = lib().pe_block_fwd(h._h, C.byref(_dims(dims)), _p(msa_in), _p(pair_in), _p(msa_mask), _p(pair_mask),
                             _p(params), _p(msa_out), _p(pair_out), _p(ctx), _p(workspace),
-                            workspace.numel() * workspace.element_size(), _s(stream_msa), _s(stream_pair))
+                            workspace.numel() * workspace.element_size(), _s(h, stream_msa), _s(h, stream_pair))
     _raise(h, rc, "pe_block_fwd", dims)
 
 
@@ -242,7 +262,7 @@ def static_scratch_bytes():
 def block_fwd_static(h, dims, msa_in, pair_in, msa_mask, pair_mask, params, msa_out, pair_out,
                      stream_msa=None, stream_pair=None):
     rc = lib().pe_block_fwd_static(h._h, C.byref(_dims(dims)), _p(msa_in), _p(pair_in), _p(msa_mask), _p(pair_mask),
-                                   _p(params), _p(msa_out), _p(pair_out), _s(stream_msa), _s(stream_pair))
+                                   _p(params), _p(msa_out), _p(pair_out), _s(h, stream_msa), _s(h, stream_pair))
     _raise(h, rc, "pe_block_fwd_static", dims)
 
 
@@ -251,7 +271,7 @@ def block_bwd(h, dims, msa_in, pair_in, msa_mask, pair_mask, params, d_msa_out, 
     rc = lib().pe_block_bwd(h._h, C.byref(_dims(dims)), _p(msa_in), _p(pair_in), _p(msa_mask), _p(pair_mask),
                             _p(params), _p(d_msa_out), _p(d_pair_out), _p(d_msa_in), _p(d_pair_in), _p(d_params),
                             _p(ctx), _p(workspace), workspace.numel() * workspace.element_size(),
-                            _s(stream_msa), _s(stream_pair))
+                            _s(h, stream_msa), _s(h, stream_pair))
     _raise(h, rc, "pe_block_bwd", dims)
 
 
@@ -264,7 +284,7 @@ def stack_fwd_bwd(h, n_extra, extra, n_main, main, extra_msa_in, msa_in, pair_in
                                 _p(extra_mask), _p(msa_mask), _p(pair_mask), _p(params), _p(d_msa_out),
                                 _p(d_pair_out), _p(msa_out), _p(pair_out), _p(d_extra_msa_in), _p(d_msa_in),
                                 _p(d_pair_in), _p(d_params), _p(workspace),
-                                workspace.numel() * workspace.element_size(), _s(stream_msa), _s(stream_pair))
+                                workspace.numel() * workspace.element_size(), _s(h, stream_msa), _s(h, stream_pair))
     _raise(h, rc, "pe_stack_fwd_bwd")
 
 
@@ -350,7 +370,7 @@ def layernorm_fwd(h, x, gain, offset, y, eps=1e-5, add=None, stats=None, ckpt=No
     _op(h, lib().pe_layernorm_fwd(
         h._h, rows, c, d, x.data_ptr(), ld, None if add is None else add.data_ptr(), lda, _vec(h, gain, c, "gain"),
         _vec(h, offset, c, "offset"), eps, y.data_ptr(), ldy, _vec(h, stats, 2 * rows, "stats"),
-        None if ckpt is None else _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), _s(stream)), "pe_layernorm_fwd")
+        None if ckpt is None else _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), _s(h, stream)), "pe_layernorm_fwd")
 
 
 def layernorm_workspace_bytes(rows, c):
@@ -374,7 +394,7 @@ def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=No
         h._h, rows, c, d, PE_CKPT if kept else d, px, ldx, _vec(h, stats, 2 * rows, "stats"), _vec(h, gain, c, "gain"),
         dy.data_ptr(), ldy, None if add is None else add.data_ptr(), lda, None if dx is None else dx.data_ptr(), ldd,
         _vec(h, d_gain, c, "d_gain"), _vec(h, d_offset, c, "d_offset"), int(accumulate), _bytes(h, workspace, 0, "workspace"),
-        ws, _s(stream)), "pe_layernorm_bwd")
+        ws, _s(h, stream)), "pe_layernorm_bwd")
 
 
 def ckpt_bytes(rows, c):
@@ -384,13 +404,13 @@ def ckpt_bytes(rows, c):
 def ckpt_pack(h, x, ckpt, stream=None):
     """x [..., c] in 8 bits into the uint8 tensor ckpt (ckpt_bytes(rows, c) bytes)."""
     d, rows, c, ld = _rows(h, x, "x")
-    _op(h, lib().pe_ckpt_pack(h._h, rows, c, d, x.data_ptr(), ld, _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), _s(stream)),
+    _op(h, lib().pe_ckpt_pack(h._h, rows, c, d, x.data_ptr(), ld, _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), _s(h, stream)),
         "pe_ckpt_pack")
 
 
 def ckpt_unpack(h, ckpt, y, stream=None):
     d, rows, c, ld = _rows(h, y, "y")
-    _op(h, lib().pe_ckpt_unpack(h._h, rows, c, d, _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), y.data_ptr(), ld, _s(stream)),
+    _op(h, lib().pe_ckpt_unpack(h._h, rows, c, d, _bytes(h, ckpt, ckpt_bytes(rows, c), "ckpt"), y.data_ptr(), ld, _s(h, stream)),
         "pe_ckpt_unpack")
 
 
@@ -437,7 +457,7 @@ def relpos_fwd(h, pos_q, pos_k, edges, table, out, seg_q=None, seg_k=None, add=N
         if add.dtype != out.dtype or add.shape != out.shape or (add.stride() != out.stride() and not (add.is_contiguous() and out.is_contiguous())):
             raise PEError("add: laid out as out is wanted")
     _op(h, lib().pe_relpos_fwd(h._h, C.byref(p), *ptr, _vec(h, table, n, "table"), None if add is None else add.data_ptr(),
-                               out.data_ptr(), _s(stream)), "pe_relpos_fwd")
+                               out.data_ptr(), _s(h, stream)), "pe_relpos_fwd")
 
 
 def relpos_workspace_bytes(n_q, n_k, c, buckets, layout="pair"):
@@ -453,5 +473,5 @@ def relpos_bwd(h, pos_q, pos_k, edges, d_out, d_table, workspace, seg_q=None, se
     """d_table [buckets, c] = sum of d_out over the pairs of each bucket."""
     p, ptr, n = _relpos(h, pos_q, pos_k, edges, d_out, seg_q, seg_k, layout, "d_out")
     _op(h, lib().pe_relpos_bwd(h._h, C.byref(p), *ptr, d_out.data_ptr(), _vec(h, d_table, n, "d_table"), int(accumulate),
-                               _bytes(h, workspace, 0, "workspace"), workspace.nbytes, _s(stream)),
+                               _bytes(h, workspace, 0, "workspace"), workspace.nbytes, _s(h, stream)),
         "pe_relpos_bwd")
