@@ -472,6 +472,8 @@ def relpos_workspace_bytes(n_q, n_k, c, buckets, layout="pair"):
 def relpos_bwd(h, pos_q, pos_k, edges, d_out, d_table, workspace, seg_q=None, seg_k=None, layout="pair", accumulate=False, stream=None):
     """d_table [buckets, c] = sum of d_out over the pairs of each bucket."""
     p, ptr, n = _relpos(h, pos_q, pos_k, edges, d_out, seg_q, seg_k, layout, "d_out")
+    if workspace is None:
+        raise PEError("workspace: relpos_workspace_bytes bytes are wanted")
     _op(h, lib().pe_relpos_bwd(h._h, C.byref(p), *ptr, d_out.data_ptr(), _vec(h, d_table, n, "d_table"), int(accumulate),
                                _bytes(h, workspace, 0, "workspace"), workspace.nbytes, _s(h, stream)),
         "pe_relpos_bwd")

@@ -77,3 +77,9 @@ def test_calls_without_a_stream_run_on_the_current_one(monkeypatch):
             call(*s)
             assert _streams(rec.calls[-1][1])[-2:] == want, rec.calls[-1][0]
     assert set(seen) == {-1}
+
+
+def test_relpos_backward_without_a_workspace_is_refused():
+    i = lambda n: torch.zeros(n, dtype=torch.int32)
+    with pytest.raises(pe.PEError, match="workspace"):
+        pe.relpos_bwd(HOST, i(4), i(3), i(1), torch.zeros(4, 3, 8), torch.zeros(2, 8), None)
