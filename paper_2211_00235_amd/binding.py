@@ -454,7 +454,10 @@ def relpos_fwd(h, pos_q, pos_k, edges, table, out, seg_q=None, seg_k=None, add=N
     p, ptr, n = _relpos(h, pos_q, pos_k, edges, out, seg_q, seg_k, layout, "out")
     if add is not None:
         _on(h, add, "add")
-        if add.dtype != out.dtype or add.shape != out.shape or (add.stride() != out.stride() and not (add.is_contiguous() and out.is_contiguous())):
+        same = add.dtype == out.dtype and add.shape == out.shape
+        if same and add.stride() != out.stride() and not (add.is_contiguous() and out.is_contiguous()):
+            same = all(a == o or n < 2 for a, o, n in zip(add.stride(), out.stride(), out.shape))      # of an axis of one element: any
+        if not same:
             raise PEError("add: laid out as out is wanted")
     _op(h, lib().pe_relpos_fwd(h._h, C.byref(p), *ptr, _vec(h, table, n, "table"), None if add is None else add.data_ptr(),
                                out.data_ptr(), _s(h, stream)), "pe_relpos_fwd")

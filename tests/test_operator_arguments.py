@@ -83,3 +83,20 @@ def test_relpos_backward_without_a_workspace_is_refused():
     i = lambda n: torch.zeros(n, dtype=torch.int32)
     with pytest.raises(pe.PEError, match="workspace"):
         pe.relpos_bwd(HOST, i(4), i(3), i(1), torch.zeros(4, 3, 8), torch.zeros(2, 8), None)
+
+
+def test_relpos_add_laid_out_as_out(monkeypatch):
+    """One row of a bias, [c][1][k] with gaps between the heads: the stride of the axis of one element may be any."""
+    rec = _Recorder()
+    monkeypatch.setattr(binding, "lib", lambda: rec)
+    h = SimpleNamespace(device=-1, _h=None, last_error=lambda: "")
+    i, bias = (lambda n: torch.zeros(n, dtype=torch.int32)), torch.zeros(6, 5, 40)
+    call = lambda out, add: pe.relpos_fwd(h, i(out.shape[1]), i(40), i(1), torch.zeros(2, 6), out, add=add, layout="heads")
+    row, same = bias[:, 2:3], torch.zeros(6, 200)[:, :40].as_strided((6, 1, 40), (200, 200, 1))
+    assert row.stride() != same.stride()
+    call(row, same)
+    call(same, row)
+    assert len(rec.calls) == 2 and rec.calls[0][1][0] is None
+    for out, add in ((row, torch.zeros(6, 1, 40)), (row, torch.zeros(6, 7, 40)[:, 2:3]), (bias, bias.transpose(0, 1).contiguous().transpose(0, 1)), (row, same.bfloat16()), (row, bias[:, 2:4])):
+        with pytest.raises(pe.PEError, match="add"):
+            call(out, add)
