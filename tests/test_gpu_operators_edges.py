@@ -138,3 +138,103 @@ def test_block_without_streams_follows_the_current_one():
         got = both()
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Relative positions, pair layout, rows with gaps: the gradient's kernel without the matrix unit, whose variants go with the channels
+# (9..16: four positions per wave, 17..32: two, more: one and slabs of 64 channels) and whose waves go with the buckets (256: two)
+CLIP, LOG = list(range(-31, 33)), [-90, -31, -15, -7, -2, -1, 0, 1, 2, 3, 8, 16, 32, 91]
+MANY = [3 * i - 381 for i in range(254)]
+
+
+def rp_inputs(rng, n_q, n_k, edges, segs, c):
+    """Positions in ascending order (runs of a bucket) for odd counts, in any order for even ones."""
+    span = max(4, n_q + n_k)
+    pos = lambda n: torch.from_numpy(np.sort(rng.integers(-span, span, n)) if n % 2 else rng.integers(-span, span, n)).int().cuda()
+    seg = lambda n: torch.from_numpy(rng.integers(0, 3, n)).int().cuda()
+    pq, pk = pos(n_q), pos(n_k)
+    sq, sk = (seg(n_q), seg(n_k)) if segs else (None, None)
+    nb = len(edges) + (2 if segs else 1)
+    b = ref.buckets(pq.cpu().numpy(), pk.cpu().numpy(), edges, *(t.cpu().numpy() if segs else None for t in (sq, sk)))
+    table = torch.from_numpy(rng.normal(size=(nb, c))).float().cuda()
+    return pq, pk, torch.tensor(edges, dtype=torch.int32), sq, sk, table, b, nb
+
+
+def rp_check(h, dt, rng, inputs, view, c):
+    """Forward into the view, in place onto it, and the gradient of what is in it: whole numbers exactly, normal ones as a sum of n
+    terms with at most n / 4 + 64 additions in a row."""
+    pq, pk, ed, sq, sk, table, b, nb = inputs
+    n_q, n_k = b.shape
+    T = f64(table)
+    pe.relpos_fwd(h, pq, pk, ed, table, view, sq, sk)
+    want = ref.relpos(b, T, None, "pair")
+    assert np.array_equal(f64(view), f64(torch.from_numpy(want).float().to(dt)))
+    A = f64(view)
+    pe.relpos_fwd(h, pq, pk, ed, table, view, sq, sk, add=view)
+    want, half = ref.relpos(b, T, A, "pair"), torch.finfo(dt).eps / 2
+    assert (np.abs(f64(view) - want) <= (half * (1 + 1e-6) + U) * np.abs(want)).all()
+    ws, d = bytes_(pe.relpos_workspace_bytes(n_q, n_k, c, nb)), torch.full((nb, c), 3.0, device="cuda")
+    view.copy_(torch.from_numpy(rng.integers(-8, 9, size=(n_q, n_k, c))))
+    exact = ref.relpos_bwd(b, f64(view), nb)
+    pe.relpos_bwd(h, pq, pk, ed, view, d, ws, sq, sk)
+    assert np.array_equal(f64(d), exact)
+    pe.relpos_bwd(h, pq, pk, ed, view, d, ws, sq, sk, accumulate=True)
+    assert np.array_equal(f64(d), 2 * exact)
+    view.copy_(torch.from_numpy(rng.normal(size=(n_q, n_k, c))))
+    pe.relpos_bwd(h, pq, pk, ed, view, d, ws, sq, sk)
+    g = f64(view)
+    assert (np.abs(f64(d) - ref.relpos_bwd(b, g, nb)) <= (64 + n_q * n_k / 4) * U * ref.relpos_bwd(b, np.abs(g), nb)).all()
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("edges, segs", [(CLIP, True), (LOG, False), (MANY, True), ([], False)], ids=["clip", "log", "many", "none"])
+@pytest.mark.parametrize("c", [9, 16, 17, 24, 32, 33, 64, 65, 130])
+def test_relpos_pair_rows_with_gaps(h, c, edges, segs, dt):
+    rng = np.random.default_rng(c)
+    for n_q, n_k, gap, off in ((37, 64, 13, 0), (130, 41, 8, 0), (19, 67, 1, 3), (3, 5, 16, 1), (9, 1, 40, 0)):
+        ld = n_k * c + gap
+        buf = torch.from_numpy(rng.normal(size=n_q * ld + off + 8)).to(dt).cuda()
+        was, view = buf.clone(), torch.as_strided(buf, (n_q, n_k, c), (ld, c, 1), off)
+        rp_check(h, dt, rng, rp_inputs(rng, n_q, n_k, edges, segs, c), view, c)
+        view.copy_(torch.as_strided(was, view.shape, view.stride(), off))
+        assert torch.equal(buf, was)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
+@pytest.mark.parametrize("n_q, n_k, c", [(1, 1, 17), (1, 15, 40), (15, 1, 65), (3, 5, 130), (1, 16, 17), (4, 4, 64)])
+def test_relpos_pair_fewer_positions_than_a_batch(h, n_q, n_k, c, dt):
+    """Around 16 positions, where the matrix unit's kernel begins."""
+    rng = np.random.default_rng(c)
+    rp_check(h, dt, rng, rp_inputs(rng, n_q, n_k, CLIP, True, c), torch.empty(n_q, n_k, c, dtype=dt, device="cuda"), c)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=["fp32", "bf16"])
+def test_relpos_pair_rows_4_gb_apart(h, dt):
+    """Three rows whose offsets pass 32 bits; what lies between them is not touched, so it is not set either."""
+    ld = 1_100_000_000 if dt is torch.bfloat16 else 600_000_000
+    buf = torch.empty(2 * ld + 40 * 130 + 8, dtype=dt, device="cuda")
+    for c in (8, 16, 24, 64, 130):
+        rng = np.random.default_rng(c)
+        edge = [buf[q * ld + 40 * c:q * ld + 40 * c + 8] for q in range(3)]      # behind the rows
+        for e in edge:
+            e.fill_(5.0)
+        rp_check(h, dt, rng, rp_inputs(rng, 3, 40, CLIP, True, c), torch.as_strided(buf, (3, 40, c), (ld, c, 1)), c)
+        assert all(bool((e == 5.0).all()) for e in edge)
+
+
+def test_ckpt_of_more_workgroups_than_a_grid_row(h):
+    """2^29 + 300 rows of one channel: 2^22 workgroups and three more, items past 2^32."""
+    rows = 2 ** 29 + 300
+    x = torch.randn(rows, 1, dtype=torch.bfloat16, device="cuda")
+    y, kept = torch.full_like(x, float("nan")), bytes_(pe.ckpt_bytes(rows, 1)).fill_(0xA5)
+    pe.ckpt_pack(h, x, kept)
+    pe.ckpt_unpack(h, kept, y)
+    at = -(-rows // 256) * 256
+    for part in (slice(0, 3000), slice(2 ** 29 - 3000, rows)):
+        codes, scales, back = ref.ckpt(f64(x[part]))
+        assert np.array_equal(kept[:rows][part].cpu().numpy().view(np.int8), codes[:, 0])
+        assert np.array_equal(kept[at:at + rows][part].cpu().numpy(), scales[:, 0])
+        assert np.array_equal(f64(y[part]), back)
+    for a in range(0, rows, 2 ** 27):                        # all of them: off by at most half a step of 64 to 127
+        p, q = x[a:a + 2 ** 27].float(), y[a:a + 2 ** 27].float()
+        assert bool(((p - q).abs() <= p.abs() / 127).all()), a
