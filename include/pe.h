@@ -170,7 +170,8 @@ int pe_handle_device(const pe_handle* h);   /* the device that was current in pe
  * its bias only).  Results are bit-identical.  Measured without gain on one MI355X (the chip
  * is already full beside the pair branch's tail), hence off.
  * PE_OPT_STACK_CKPT (default 0): 1 = pe_stack_fwd_bwd saves the block inputs that it keeps for
- * the backward pass in 8 bits (pe_ckpt_pack: 33/64 of their bf16 size, 33/128 of fp32) and
+ * the backward pass in 8 bits (pe_ckpt_pack: a byte per element and one per started group of 32
+ * channels; 33/64 of the bf16 size, 33/128 of fp32, where channels are a multiple of 32) and
  * restores them in front of each block's recompute; pe_stack_workspace_bytes_ckpt bytes of
  * workspace.  Outputs are bit-identical; cotangents and gradients are those of every block but
  * the first and the last taken at its restored inputs.  Not together with PE_OPT_STACK_KEEP_CTX. */
