@@ -110,10 +110,11 @@ template <bool PACK> void ck_run(hipStream_t st, int dtype, bool whole, const vo
       const int per_row = V == 8 ? (int)ck_groups(c) * 4 : 8;
       const long long items = rows * per_row, blocks = (items + 256 * U - 1) / (256 * U);
       const dim3 grid((unsigned)std::min<long long>(blocks, CK_GRID_X), (unsigned)((blocks + CK_GRID_X - 1) / CK_GRID_X));
-      stream_dispatch(PACK ? (double)rows * c * sizeof(T) : 0.0, [&](auto nt) {
+      auto launch = [&](auto nt) {
         hipLaunchKernelGGL((ckpt_kernel<T, V, w.value, U, PACK, nt.value>), grid, dim3(256), 0, st, (const T*)x, ld, (int8_t*)ckpt,
                            (uint8_t*)ckpt + up256((size_t)rows * c), (T*)y, rows, c, per_row, (int)(c % CK_GROUP == 0 && (ld == c || rows == 1)));
-      });
+      };
+      if constexpr (PACK) stream_dispatch((double)rows * c * sizeof(T), launch); else launch(std::false_type{});
     });
   });
 }

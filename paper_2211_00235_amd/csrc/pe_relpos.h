@@ -20,7 +20,8 @@ struct RpArgs {
   float* part;
   long long ld;            // elements between rows q
   int n_q, n_k, c, nb;     // nb: buckets, the one of different segments among them
-  int n_edges, mode;       // RpMode
+  int n_edges;
+  int mode;                // RpMode, by which the host side picks the kernel
   int lo, hi;              // DENSE, LUT: first edge - 1, last edge (0, 0 without edges)
   int edges[RP_MAX_EDGES];
 };
