@@ -294,10 +294,7 @@ def stack_fwd_bwd(h, n_extra, extra, n_main, main, extra_msa_in, msa_in, pair_in
 # ---------------------------------------------------------------------------
 _DTYPES = {}      # by torch type, filled as types come
 
-
-def _int32(*sizes):
-    """Whether sizes fit the C int that they are passed as (ctypes keeps the low 32 bits, which may be a size in range)."""
-    return all(-2 ** 31 <= n < 2 ** 31 for n in sizes)
+# A size is passed as a C int, of which ctypes keeps the low 32 bits, and those may be a size in range: n >> 31 is 0 where n is one.
 
 
 def _dtype(t):
@@ -374,7 +371,7 @@ def layernorm_fwd(h, x, gain, offset, y, eps=1e-5, add=None, stats=None, ckpt=No
 
 
 def layernorm_workspace_bytes(rows, c):
-    return int(lib().pe_layernorm_workspace_bytes(rows, c)) if _int32(c) else 0
+    return 0 if c >> 31 else int(lib().pe_layernorm_workspace_bytes(rows, c))
 
 
 def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=None, accumulate=False, stream=None):
@@ -398,7 +395,7 @@ def layernorm_bwd(h, dy, x, stats, gain, dx, d_gain, d_offset, workspace, add=No
 
 
 def ckpt_bytes(rows, c):
-    return int(lib().pe_ckpt_bytes(rows, c)) if _int32(c) else 0
+    return 0 if c >> 31 else int(lib().pe_ckpt_bytes(rows, c))
 
 
 def ckpt_pack(h, x, ckpt, stream=None):
@@ -466,7 +463,7 @@ def relpos_fwd(h, pos_q, pos_k, edges, table, out, seg_q=None, seg_k=None, add=N
 def relpos_workspace_bytes(n_q, n_k, c, buckets, layout="pair"):
     """Bytes for relpos_bwd; buckets: rows of the table."""
     segments = int(buckets > 1)
-    if not _int32(n_q, n_k, c, buckets):
+    if (n_q | n_k | c | buckets) >> 31:
         return 0
     p = _Relpos(n_q, n_k, c, buckets - 1 - segments, segments, _LAYOUTS[layout], PE_F32, 0)
     return int(lib().pe_relpos_workspace_bytes(C.byref(p)))
