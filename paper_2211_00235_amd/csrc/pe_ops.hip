@@ -82,9 +82,11 @@ template <typename F> void width_dispatch(long long c, bool whole, F&& f) {
   else f(std::integral_constant<int, 8>{}, std::false_type{});
 }
 // Non-temporal loads of a tensor that a call reads once: from 32 MB on (an eighth of the memory-side cache).  With and without, us:
-// relpos pair backward 17 MB of gradients 12.9 and 11.5, 38 MB 14.8 and 17.4, 268 MB 49 and 78; packing and restoring 17 MB 13.5 and
-// 13.1, 252 MB 134 and 141.  Layer norm stays without: its backward pass finds part of what the forward pass has read (29 MB fp32, both passes,
-// 38.2 and 34.5, 67 MB bf16 90.1 and 87.6).
+// relpos pair backward 17 MB of gradients 12.9 and 11.5.  Behind a forward pass, which in turn finds less of itself in the cache: 67 MB
+// backward 18.2 and 23.7, forward 26.4 and 23.9, 268 MB 50.8 and 80.4, 91.8 and 78.9; both passes and the sums 38 MB 31.9 and 36.8, 67 MB 49.1 and 51.6,
+// 134 MB 81.5 and 88.1, 268 MB 146 and 160.  Heads 134 MB, both passes, 64.3 and 68.2; packing and restoring 17 MB 13.5 and
+// 13.1, 126 MB 65.0 and 74.2, 252 MB 134 and 141.  Layer norm stays without: its backward pass finds part of what the forward pass has read (29 MB fp32,
+// both passes, 38.2 and 34.5, 67 MB bf16 90.1 and 87.6).
 template <typename F> void stream_dispatch(double bytes, F&& f) {
   if (bytes >= 32e6) f(std::true_type{}); else f(std::false_type{});
 }
@@ -159,9 +161,11 @@ LnPlan ln_plan(int c) {
   if (n <= 1024) return {512, 2};
   return {1024, 2};
 }
-// Most workgroups of a launch: they walk over the rows.  Backward, each writes 8 c bytes of partial sums: as many as the chip holds at once,
-// four per CU of rows within waves, two or one of rows of whole workgroups (4096 x 8192 with 512 of them 60 us and 11 for the sums,
-// with 256 49 and 7).
+// Most workgroups of a launch: they walk over the rows.  Forward with 1024, 2048 and 4096, us: 28677 x 256 fp32 11.9, 11.6 and 11.2, 196608 x 256 bf16
+// 40.1, 39.6 and 39.6; rows of whole workgroups, which load gain and offset for a few rows only, 4096 x 8192 30.4, 31.0 and 35.8, 2048 x 16384 38.2,
+// 41.5 and 41.7.  Backward, each writes 8 c bytes of partial sums: four per CU of rows within waves (the chip holds as many up to 512 channels; of
+// 64 lanes with two vectors each, 159 and 186 registers, three in bf16 and two in fp32), two or one of rows of whole workgroups (4096 x 8192 with 512 of
+// them 60 us and 11 for the sums, with 256 49 and 7).
 constexpr int LN_FWD_WG = 2048, LN_BWD_WG = 1024;
 long long ln_bwd_groups(long long rows, int c) {
   const LnPlan p = ln_plan(c);
@@ -228,7 +232,8 @@ long long rp_pair_groups(const pe_relpos& p) {
   return std::max<long long>(1, std::min<long long>(256 / ((p.c + 63) / 64), (n + 511) / 512));
 }
 // HEADS: 64 vectors of 8 positions k (fewer than 8: of one) per workgroup; so many workgroups share the rows q of those and of a head
-// that there are about 512, with a row per wave at least
+// that there are about 512, with a row per wave at least.  That is one round of the chip where two fit a CU's LDS, up to about 38 buckets (2048 x 2048 x 16
+// with 32 buckets 33 us with the sums); with more there is one per CU, and two rounds or three (65 buckets 37.5; 1021 x 1021 x 12 30.4).
 long long rp_heads_tiles(const pe_relpos& p) { return ((p.n_k < 8 ? p.n_k : (p.n_k + 7) / 8) + 63LL) / 64; }
 int rp_heads_split(const pe_relpos& p) {
   const long long all = rp_heads_tiles(p) * p.c;
@@ -334,7 +339,10 @@ template <typename T, int V, bool WHOLE> void rp_heads_bwd(hipStream_t st, int d
     });
   });
 }
-// The matrix unit's kernel: rows without gaps, more than 16 channels, a batch of positions at least
+// The matrix unit's kernel: rows without gaps, more than 16 channels, a batch of positions at least.  384 x 384 positions with the sums, by it and by the
+// kernel without, us: bf16 8 channels 12.0 and 10.7, 16 12.3 and 11.7, 24 12.7 and 16.6, 32 12.7 and 16.3, 48 13.6 and 15.9, 128 19.2 and 21.3, with positions in
+// any order 19.7 and 29.4.  fp32 16 channels 18.0 and 11.9, 32 18.0 and 16.5, 128 26.0 and 23.7 (1024 x 1024: 93 and 98), in any order 39.0 and 30.2:
+// there the two are near one another where neighbours' distances are alike, and the kernel without is the faster one where they are not.
 bool rp_pair_mm(const RpArgs& a) { return a.c > 16 && a.ld == (long long)a.n_k * a.c && (long long)a.n_q * a.n_k >= 16; }
 template <typename T, int NB> void rp_pair_bwd_mm(hipStream_t st, int device, const RpArgs& a, long long groups) {
   rp_dispatch_few(a.mode, [&](auto m) {
@@ -501,7 +509,9 @@ int pe_relpos_fwd(pe_handle* h, const pe_relpos* p, const int* edges, const int*
     op.launch("relpos fwd", pair ? "relpos_pair_fwd_kernel" : "relpos_heads_fwd_kernel", n, n * e * (add ? 2 : 1), [&] {
       type_dispatch(p->dtype, [&](auto t) {
         using T = decltype(t);
-        // little to write: a position per lane, so that eight times the workgroups share it (1 x 8191 x 8: 3.7 us, by vectors 7.1)
+        // little to write: a position per lane, so that eight times the workgroups share it.  By positions and by vectors, us: 1 x 8191 x 8 fp32
+        // 2.9 and 6.6, 1 x 32768 x 8 3.2 and 6.3; beyond the border, where vectors are taken, 1 x 65536 x 8 3.4 and 6.6, 256 x 512 x 16 bf16 4.9 and 7.6,
+        // 1 x 524288 x 8 7.9 and 9.3
         if (!pair && n < (1 << 19)) rp_heads_fwd<T, 1, true>(op.st, a);
         else width_dispatch(pair ? p->c : p->n_k, whole, [&](auto v, auto w) {
           if (pair) rp_pair_fwd<T, v.value, w.value>(op.st, a); else rp_heads_fwd<T, v.value, w.value>(op.st, a);
